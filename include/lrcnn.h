@@ -347,6 +347,130 @@ int lrcnn_sgd_update(const lrcnn_plan_t *plan, float lr, void *const *w,
                      float *fc_b, const float *d_fc_b, int32_t n_classes,
                      void *stream);
 
+/* ---- Feed-forward blocks with 8-bit activation checkpoints. What a block keeps
+ * from its forward to its backward pass (a norm's input, a linear layer's
+ * input, an activation's input) is held in 8 bits a value, and the backward
+ * pass reads that. The block's linear products and input gradients are 1x1
+ * convolutions (plans above).
+ *
+ * Further conventions of these entry points:
+ *  - A matrix is row-major, `rows` x `cols`, with a row stride ld* in elements
+ *    (0: cols, else >= cols). Storage type: `dtype` (float32 or bfloat16).
+ *    Matrices and float32 vectors need only their element's alignment;
+ *    checkpoints and workspaces 16 bytes. Any width from 1 on, any number of
+ *    rows from 0 on.
+ *  - An output may be an input of the same call only where both are the same
+ *    matrix (pointer, stride and type); other overlaps are not allowed.
+ *  - Sums, statistics and activations are computed in float32 and rounded once.
+ *    Every sum runs in a fixed order: results are reproducible run to run.
+ *  - accumulate != 0: weight gradients are added to what is there (bands,
+ *    micro-batches), else overwritten.
+ *  - Errors: EINVAL (null or misaligned pointer, arguments that do not go
+ *    together), ESHAPE, EDTYPE, EWORKSPACE, EHIP. Nothing is enqueued by a
+ *    call that refuses its arguments.
+ *
+ * The checkpoint of a matrix is one buffer of lrcnn_act8_bytes bytes:
+ * codes int8 [rows][pitch], pitch = cols rounded up to 32 (zeros behind the
+ * last column); then, from the next multiple of 256 bytes, exponent bytes
+ * [rows][pitch / 32], one for each group of 32 columns. With m the group's
+ * largest magnitude and bits(m) its float32 bits,
+ *   E = max((bits(m) + 2^16) >> 23, 7),  code = rint(x * 2^(133 - E)),
+ * the code (ties to even) within [-127, 127], and the value stands for
+ * code * 2^(E - 133): within 2^(E - 134) of x. E is at most 254 (codes are then
+ * held to +-127); a group with an infinity or a NaN has E = 255, codes 0, and
+ * stands for NaN. The values are exact in bfloat16 and float32. */
+
+/* Bytes of the checkpoint of a rows x cols matrix. */
+int lrcnn_act8_bytes(int64_t rows, int64_t cols, size_t *bytes);
+
+/* Checkpoint of x. */
+int lrcnn_act8_pack(int64_t rows, int64_t cols, int32_t dtype, const void *x,
+                    int64_t ldx, void *ckpt, void *stream);
+
+/* y = what the checkpoint stands for (in `dtype`, whatever it was packed
+ * from). */
+int lrcnn_act8_unpack(int64_t rows, int64_t cols, int32_t dtype,
+                      const void *ckpt, void *y, int64_t ldy, void *stream);
+
+/* Layer norm of each row: t = x, or x + residual rounded to the storage type
+ * (written to `total` where not NULL);
+ *   xh = (t - mean) * rstd, rstd = 1 / sqrt(var + eps), y = gamma * xh + beta.
+ * gamma, beta: float32 [cols], NULL for 1 and 0. mean, rstd: float32 [rows],
+ * nullable. ckpt (nullable): receives the checkpoint of xh, which serves both
+ * lrcnn_layer_norm_backward and, with gamma and beta as scale and shift, the
+ * lrcnn_linear_wgrad of a linear layer that reads y. cols <= 16384. */
+int lrcnn_layer_norm_forward(int64_t rows, int64_t cols, int32_t dtype,
+                             const void *x, int64_t ldx, const void *residual,
+                             int64_t ldr, const float *gamma, const float *beta,
+                             float eps, void *total, int64_t ldt, void *y,
+                             int64_t ldy, float *mean, float *rstd, void *ckpt,
+                             void *stream);
+
+/* Device scratch bytes of lrcnn_layer_norm_backward. */
+int lrcnn_layer_norm_workspace_bytes(int64_t rows, int64_t cols, size_t *bytes);
+
+/* Gradients of the layer norm from dy = dL/dy and either its input x (the sum
+ * with the residual, where there was one) with mean, or ckpt; and rstd:
+ *   g = gamma * dy, dx = rstd * (g - mean(g) - xh * mean(g * xh)) [+ dres],
+ *   dgamma = sum over rows of dy * xh, dbeta = sum over rows of dy.
+ * dres (nullable): the gradient that reaches t past the norm. dgamma, dbeta:
+ * float32 [cols], each nullable (workspace may be NULL if both are). */
+int lrcnn_layer_norm_backward(int64_t rows, int64_t cols, int32_t dtype,
+                              const void *dy, int64_t lddy, const void *x,
+                              int64_t ldx, const float *mean, const void *ckpt,
+                              const float *rstd, const float *gamma,
+                              const void *dres, int64_t lddr, void *dx,
+                              int64_t lddx, float *dgamma, float *dbeta,
+                              int32_t accumulate, void *workspace,
+                              size_t ws_bytes, void *stream);
+
+/* Activations: relu; gelu, x * Phi(x); its tanh form; silu, x / (1 + e^-x). */
+enum {
+  LRCNN_ACT_RELU = 0,
+  LRCNN_ACT_GELU = 1,
+  LRCNN_ACT_GELU_TANH = 2,
+  LRCNN_ACT_SILU = 3
+};
+
+/* a = f(u), or f(u) * v where v is not NULL (gated). Writes any of a and the
+ * checkpoints of u, v and a (nullable, at least one given; the checkpoint of a
+ * is formed from its float32 value). */
+int lrcnn_activation_forward(int64_t rows, int64_t cols, int32_t dtype,
+                             int32_t kind, const void *u, int64_t ldu,
+                             const void *v, int64_t ldv, void *a, int64_t lda,
+                             void *ckpt_u, void *ckpt_v, void *ckpt_a,
+                             void *stream);
+
+/* du = da * f'(u) [* v], dv = da * f(u), from u (and v), or from their
+ * checkpoints in place of them. ckpt_a (nullable): receives the checkpoint of
+ * f(u) [* v], the input of the linear layer behind the activation, for
+ * its lrcnn_linear_wgrad. f'(0) of relu is 0. */
+int lrcnn_activation_backward(int64_t rows, int64_t cols, int32_t dtype,
+                              int32_t kind, const void *da, int64_t ldda,
+                              const void *u, int64_t ldu, const void *v,
+                              int64_t ldv, const void *ckpt_u,
+                              const void *ckpt_v, void *du, int64_t lddu,
+                              void *dv, int64_t lddv, void *ckpt_a,
+                              void *stream);
+
+/* Device scratch bytes of lrcnn_linear_wgrad (0: none, NULL will do). */
+int lrcnn_linear_wgrad_workspace_bytes(int64_t rows, int64_t n_in,
+                                       int64_t n_out, int32_t dtype,
+                                       size_t *bytes);
+
+/* Weight and bias gradient of a linear layer y = x W^T + b, W [n_out][n_in],
+ * from dy = dL/dy (rows x n_out) and a checkpoint (rows x n_in) of q with
+ * x = scale * q + shift per column (float32 [n_in], NULL for 1 and 0):
+ *   dw[n][k] = sum over rows of dy[.][n] * x[.][k]   (float32, dense)
+ *   db[n]    = sum over rows of dy[.][n]             (float32, nullable)
+ * Products are exact, sums float32, for either dtype of dy. */
+int lrcnn_linear_wgrad(int64_t rows, int64_t n_in, int64_t n_out,
+                       int32_t dtype, const void *dy, int64_t lddy,
+                       const void *ckpt, const float *scale,
+                       const float *shift, float *dw, float *db,
+                       int32_t accumulate, void *workspace, size_t ws_bytes,
+                       void *stream);
+
 /* Message of the last failed call on this thread ("" if none). */
 const char *lrcnn_last_error(void);
 

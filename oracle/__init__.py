@@ -15,6 +15,8 @@ Modules:
   brute   -- scalar loops for tiny shapes that pin ``column``
   head    -- classifier head, softmax cross-entropy and SGD of a full training
              step (Algorithm 1's fully connected FP/BP, loss and update)
+  block   -- 8-bit activation checkpoints, layer norm, activations and the
+             linear layer's weight gradient of a feed-forward block
 
 Parity status: every function is pinned by tests in ``tests/test_oracle_*``
 (brute force, library routines, adjoint identities, finite differences,

@@ -25,6 +25,7 @@ F32, BF16 = 0, 1
 CARRY, RECOMPUTE = 0, 1
 EVEN, BALANCED, EXPLICIT, PAPER_2PS = 0, 1, 2, 3
 HYBRID_AUTO = -1
+ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3
 
 STATUS = {0: "OK", -1: "EINVAL", -2: "ESHAPE", -3: "EPARTITION",
           -4: "EWORKSPACE", -5: "ESTATE", -6: "EDTYPE", -7: "EHIP",
@@ -74,6 +75,13 @@ class Budget(C.Structure):
                 ("max_refine", C.c_int32), ("want_dx", C.c_int32)]
 
 
+_BLOCK_EXPORTS = ("lrcnn_act8_bytes", "lrcnn_act8_pack", "lrcnn_act8_unpack",
+                  "lrcnn_layer_norm_forward", "lrcnn_layer_norm_workspace_bytes",
+                  "lrcnn_layer_norm_backward", "lrcnn_activation_forward",
+                  "lrcnn_activation_backward", "lrcnn_linear_wgrad_workspace_bytes",
+                  "lrcnn_linear_wgrad")
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(
@@ -101,6 +109,22 @@ def _load():
     lib.lrcnn_head_workspace_bytes.argtypes = [vp, i32, C.POINTER(sz)]
     lib.lrcnn_head_loss.argtypes = [vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.lrcnn_sgd_update.argtypes = [vp, C.c_float, pp, pp, vp, vp, vp, vp, i32, vp]
+    i64, f32, psz = C.c_int64, C.c_float, C.POINTER(sz)
+    lib.lrcnn_act8_bytes.argtypes = [i64, i64, psz]
+    lib.lrcnn_act8_pack.argtypes = [i64, i64, i32, vp, i64, vp, vp]
+    lib.lrcnn_act8_unpack.argtypes = [i64, i64, i32, vp, vp, i64, vp]
+    lib.lrcnn_layer_norm_forward.argtypes = [i64, i64, i32, vp, i64, vp, i64, vp, vp, f32, vp,
+                                             i64, vp, i64, vp, vp, vp, vp]
+    lib.lrcnn_layer_norm_workspace_bytes.argtypes = [i64, i64, psz]
+    lib.lrcnn_layer_norm_backward.argtypes = [i64, i64, i32, vp, i64, vp, i64, vp, vp, vp, vp,
+                                              vp, i64, vp, i64, vp, vp, i32, vp, sz, vp]
+    lib.lrcnn_activation_forward.argtypes = [i64, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp,
+                                             vp, vp, vp]
+    lib.lrcnn_activation_backward.argtypes = [i64, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp,
+                                              vp, vp, i64, vp, i64, vp, vp]
+    lib.lrcnn_linear_wgrad_workspace_bytes.argtypes = [i64, i64, i64, i32, psz]
+    lib.lrcnn_linear_wgrad.argtypes = [i64, i64, i64, i32, vp, i64, vp, vp, vp, vp, vp, i32, vp,
+                                       sz, vp]
     lib.lrcnn_last_error.restype = C.c_char_p
     lib.lrcnn_debug_dry_run.argtypes = [C.c_int]
     lib.lrcnn_debug_dry_run.restype = None
@@ -131,7 +155,7 @@ def _load():
               "lrcnn_backward_rows",
               "lrcnn_layerwise_reference_gpu", "lrcnn_plan_step_bytes",
               "lrcnn_plan_for_budget", "lrcnn_max_batch", "lrcnn_head_workspace_bytes",
-              "lrcnn_head_loss", "lrcnn_sgd_update"):
+              "lrcnn_head_loss", "lrcnn_sgd_update", *_BLOCK_EXPORTS):
         getattr(lib, f).restype = C.c_int
     return lib
 
@@ -151,7 +175,7 @@ EXPORTS = ("lrcnn_plan", "lrcnn_plan_query", "lrcnn_plan_node_shape",
            "lrcnn_debug_profile",
            "lrcnn_debug_profile_collect", "lrcnn_debug_profile_entry",
            "lrcnn_debug_profile_roofline",
-           "lrcnn_debug_layerwise_map")
+           "lrcnn_debug_layerwise_map", *_BLOCK_EXPORTS)
 
 
 def _check(code):
@@ -321,6 +345,187 @@ def lrcnn_sgd_update(plan, lr, weights, dws, fc_w=None, d_fc_w=None, fc_b=None, 
     _check(LIB.lrcnn_sgd_update(
         plan.handle, C.c_float(lr), _ptr_array(weights), _ptr_array(dws), _ptr(fc_w),
         _ptr(d_fc_w), _ptr(fc_b), _ptr(d_fc_b), n_classes, _stream(stream)))
+
+
+# ---- feed-forward blocks with 8-bit activation checkpoints (2-d tensors of one
+# dtype and device, columns next to each other, rows at any stride). The tensors'
+# shapes give the sizes; ones that do not agree are refused before the call.
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _einval(msg):
+    raise LrcnnError(-1, msg)
+
+
+def _dtype_of(name, t):
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise LrcnnError(-6, f"{name}: dtype must be float32 or bfloat16")
+    return code
+
+
+def _mat(name, t, like):
+    """Pointer and row stride of a matrix of like's shape, dtype and device (None:
+    absent)."""
+    if t is None:
+        return None, 0
+    if t.shape != like.shape or t.dtype != like.dtype or t.device != like.device:
+        _einval(f"{name} must be a matrix like {tuple(like.shape)} {like.dtype} on {like.device}")
+    ld, one = t.stride()
+    rows, cols = t.shape
+    if (one != 1 and cols > 1) or (ld < cols and rows > 1):
+        _einval(f"{name}: columns must be next to each other, rows apart")
+    return t.data_ptr(), ld if rows > 1 else 0
+
+
+def _shape(name, t):
+    if t.dim() != 2:
+        _einval(f"{name} must have two dimensions")
+    if t.shape[1] < 1:
+        raise LrcnnError(-2, f"{name} has no columns")
+    return t.shape
+
+
+def _vec(name, t, n, like):
+    """Pointer of a dense float32 vector of n elements (None: absent)."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous() \
+            or t.device != like.device:
+        _einval(f"{name} must be {n} dense float32 values on {like.device}")
+    return t.data_ptr()
+
+
+def _bytes(name, t, need, like, code):
+    """Pointer of a byte buffer of at least `need` bytes (None: absent)."""
+    if t is None:
+        return None
+    if t.dtype != torch.uint8 or not t.is_contiguous() or t.device != like.device:
+        _einval(f"{name} must be dense uint8 on {like.device}")
+    if t.numel() < need:
+        raise LrcnnError(code, f"{name} needs {need} bytes, got {t.numel()}")
+    return t.data_ptr()
+
+
+def _ckpt(name, t, shape, like):
+    if t is None:
+        return None
+    return _bytes(name, t, lrcnn_act8_bytes(*shape), like, -1)
+
+
+def _query(fn, *args):
+    out = C.c_size_t()
+    _check(fn(*args, C.byref(out)))
+    return out.value
+
+
+def lrcnn_act8_bytes(rows, cols):
+    """Bytes of the 8-bit checkpoint of a rows x cols matrix."""
+    return _query(LIB.lrcnn_act8_bytes, rows, cols)
+
+
+def lrcnn_act8_pack(x, ckpt, stream=None):
+    """ckpt (uint8, lrcnn_act8_bytes) = the 8-bit checkpoint of x."""
+    rows, cols = _shape("x", x)
+    dt, (px, ldx) = _dtype_of("x", x), _mat("x", x, x)
+    _check(LIB.lrcnn_act8_pack(rows, cols, dt, px, ldx, _ckpt("ckpt", ckpt, x.shape, x),
+                               _stream(stream)))
+
+
+def lrcnn_act8_unpack(ckpt, y, stream=None):
+    """y = what the checkpoint of a matrix of y's shape stands for."""
+    rows, cols = _shape("y", y)
+    dt, (py, ldy) = _dtype_of("y", y), _mat("y", y, y)
+    _check(LIB.lrcnn_act8_unpack(rows, cols, dt, _ckpt("ckpt", ckpt, y.shape, y), py, ldy,
+                                 _stream(stream)))
+
+
+def lrcnn_layer_norm_forward(x, gamma, beta, eps, y, residual=None, total=None, mean=None,
+                             rstd=None, ckpt=None, stream=None):
+    """y = layer norm of the rows of x (+ residual: their sum goes to total);
+    mean, rstd per row; ckpt: the checkpoint of the normalised rows."""
+    rows, cols = _shape("x", x)
+    dt, (px, ldx) = _dtype_of("x", x), _mat("x", x, x)
+    pr, ldr = _mat("residual", residual, x)
+    pt, ldt = _mat("total", total, x)
+    py, ldy = _mat("y", y, x)
+    _check(LIB.lrcnn_layer_norm_forward(
+        rows, cols, dt, px, ldx, pr, ldr, _vec("gamma", gamma, cols, x),
+        _vec("beta", beta, cols, x), eps, pt, ldt, py, ldy, _vec("mean", mean, rows, x),
+        _vec("rstd", rstd, rows, x), _ckpt("ckpt", ckpt, x.shape, x), _stream(stream)))
+
+
+def lrcnn_layer_norm_workspace_bytes(rows, cols):
+    return _query(LIB.lrcnn_layer_norm_workspace_bytes, rows, cols)
+
+
+def lrcnn_layer_norm_backward(dy, rstd, gamma, dx, dgamma=None, dbeta=None, workspace=None,
+                              x=None, mean=None, ckpt=None, dres=None, accumulate=False,
+                              stream=None):
+    """dx (+ dres), dgamma and dbeta from dy and either (x, mean) or ckpt."""
+    rows, cols = _shape("dy", dy)
+    dt, (pdy, lddy) = _dtype_of("dy", dy), _mat("dy", dy, dy)
+    px, ldx = _mat("x", x, dy)
+    pr, ldr = _mat("dres", dres, dy)
+    pdx, lddx = _mat("dx", dx, dy)
+    _check(LIB.lrcnn_layer_norm_backward(
+        rows, cols, dt, pdy, lddy, px, ldx, _vec("mean", mean, rows, dy),
+        _ckpt("ckpt", ckpt, dy.shape, dy), _vec("rstd", rstd, rows, dy),
+        _vec("gamma", gamma, cols, dy), pr, ldr, pdx, lddx, _vec("dgamma", dgamma, cols, dy),
+        _vec("dbeta", dbeta, cols, dy), 1 if accumulate else 0,
+        _bytes("workspace", workspace, 0, dy, -4),
+        0 if workspace is None else workspace.numel(), _stream(stream)))
+
+
+def lrcnn_activation_forward(kind, u, a=None, v=None, ckpt_u=None, ckpt_v=None, ckpt_a=None,
+                             stream=None):
+    """a = f(u) (times v), and the checkpoints of u, v and a that are given."""
+    rows, cols = _shape("u", u)
+    dt, (pu, ldu) = _dtype_of("u", u), _mat("u", u, u)
+    pv, ldv = _mat("v", v, u)
+    pa, lda = _mat("a", a, u)
+    _check(LIB.lrcnn_activation_forward(
+        rows, cols, dt, kind, pu, ldu, pv, ldv, pa, lda, _ckpt("ckpt_u", ckpt_u, u.shape, u),
+        _ckpt("ckpt_v", ckpt_v, u.shape, u), _ckpt("ckpt_a", ckpt_a, u.shape, u),
+        _stream(stream)))
+
+
+def lrcnn_activation_backward(kind, da, du, u=None, v=None, ckpt_u=None, ckpt_v=None, dv=None,
+                              ckpt_a=None, stream=None):
+    """du (and dv) from da and either u (and v) or their checkpoints; ckpt_a:
+    receives the checkpoint of the activation's output."""
+    rows, cols = _shape("da", da)
+    dt, (pda, ldda) = _dtype_of("da", da), _mat("da", da, da)
+    pu, ldu = _mat("u", u, da)
+    pv, ldv = _mat("v", v, da)
+    pdu, lddu = _mat("du", du, da)
+    pdv, lddv = _mat("dv", dv, da)
+    _check(LIB.lrcnn_activation_backward(
+        rows, cols, dt, kind, pda, ldda, pu, ldu, pv, ldv,
+        _ckpt("ckpt_u", ckpt_u, da.shape, da), _ckpt("ckpt_v", ckpt_v, da.shape, da), pdu, lddu,
+        pdv, lddv, _ckpt("ckpt_a", ckpt_a, da.shape, da), _stream(stream)))
+
+
+def lrcnn_linear_wgrad_workspace_bytes(rows, n_in, n_out, dtype=F32):
+    return _query(LIB.lrcnn_linear_wgrad_workspace_bytes, rows, n_in, n_out, dtype)
+
+
+def lrcnn_linear_wgrad(dy, ckpt, dw, workspace=None, db=None, scale=None, shift=None,
+                       accumulate=False, stream=None):
+    """dw [n_out][n_in] and db [n_out] of a linear layer from dy [rows][n_out] and
+    the checkpoint [rows][n_in] of its input (the input being scale times that
+    plus shift, per column)."""
+    rows, n_out = _shape("dy", dy)
+    dt, (pdy, lddy) = _dtype_of("dy", dy), _mat("dy", dy, dy)
+    if dw.dim() != 2 or dw.shape[0] != n_out:
+        _einval("dw must be [n_out][n_in]")
+    n_in = _shape("dw", dw)[1]
+    _check(LIB.lrcnn_linear_wgrad(
+        rows, n_in, n_out, dt, pdy, lddy, _ckpt("ckpt", ckpt, (rows, n_in), dy),
+        _vec("scale", scale, n_in, dy), _vec("shift", shift, n_in, dy),
+        _vec("dw", dw, n_out * n_in, dy), _vec("db", db, n_out, dy), 1 if accumulate else 0,
+        _bytes("workspace", workspace, 0, dy, -4),
+        0 if workspace is None else workspace.numel(), _stream(stream)))
 
 
 def lrcnn_debug_dry_run(on):
