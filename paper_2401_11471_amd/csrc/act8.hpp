@@ -115,9 +115,10 @@ __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(bf16 *p, float v) {
   *p = __builtin_bit_cast(bf16, (__bf16)v);
 }
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t bf_pair(float a, float b) {
-  return (uint32_t)__builtin_bit_cast(bf16, (__bf16)a) |
-         ((uint32_t)__builtin_bit_cast(bf16, (__bf16)b) << 16);
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2));
 }
 
 // What a thread holds of a row: eight columns as stored.

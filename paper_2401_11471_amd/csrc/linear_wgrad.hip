@@ -21,12 +21,12 @@ namespace lrcnn {
 namespace act8 {
 namespace {
 
-constexpr int kTile = 128, kStep = 32;  // tile of dW (n and k), rows per step
+constexpr int kStep = 32;  // rows of dy and of the checkpoint per step
 
 struct WgArgs {
   int64_t rows;
   int n, k;             // outputs, inputs
-  int64_t chunk;        // rows per split
+  int64_t chunk;        // rows per split, a multiple of kStep
   Mat dy;
   Ckpt q;
   const float *scale, *shift;
@@ -42,119 +42,229 @@ __device__ __forceinline__ void cut3(float v, float (&p)[3]) {
   p[1] = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
   p[2] = r - p[1];
 }
+__device__ __forceinline__ uint4 bf_vec(const float *v) {
+  return make_uint4(bf_pair(v[0], v[1]), bf_pair(v[2], v[3]), bf_pair(v[4], v[5]),
+                    bf_pair(v[6], v[7]));
+}
 
-template <typename T>
-__global__ __launch_bounds__(256, 2) void wgrad8_kernel(WgArgs a) {
-  constexpr int P = std::is_same<T, float>::value ? 3 : 1;
-  using M = KM<bf16, kTile>;
-  __shared__ __align__(16) bf16 As[2][P][kStep * kTile];
-  __shared__ __align__(16) bf16 Bs[2][kStep * kTile];
-  __shared__ float dbs[kTile];
+// Tiles run through a panel of eight tiles of n before the next k, so that
+// the run of tiles an XCD works on shares rows of both operands in its L2.
+__device__ __forceinline__ TileId panel_tile() {
+  const int gx = gridDim.x, gy = gridDim.y;
+  TileId t = xcd_tile(false);
+  const int id = t.x + gx * t.y, panel = id / (8 * gy), r = id - panel * 8 * gy;
+  const int w = min(8, gx - 8 * panel);
+  t.y = r / w;
+  t.x = 8 * panel + (r - t.y * w);
+  return t;
+}
+
+// A W x W tile of S by four waves of W/2 x W/2. Both operands go through
+// registers into k-major LDS tiles (the codes as bfloat16, dy as it is or in
+// three pieces), and to the matrix cores by transposing reads. A step's loads
+// are issued RS steps before its tile is written to LDS, the tile is written
+// one step before it is multiplied, and a unit's fragments (16 rows; one
+// piece of dy) are read one unit before their MFMAs.
+template <typename T, int W>
+__global__ __launch_bounds__(256, W == 256 ? 1 : 2) void wgrad8_kernel(WgArgs a) {
+  constexpr int P = std::is_same<T, float>::value ? 3 : 1;  // pieces of dy
+  constexpr int ST = P == 1 ? 3 : 2;                         // LDS tiles and load slots
+  constexpr int NB = W / 64;                                 // 32 x 32 blocks per wave and side
+  constexpr int U = 2 * P;                                   // units per step
+  constexpr int LA = W / 8, RA = 256 / LA, NA = kStep / RA;  // dy: lanes, rows, passes
+  constexpr int LB = W / 16, RB = 256 / LB, NQ = kStep / RB; // codes
+  using M = KM<bf16, W>;
+  constexpr int TS = kStep * W;  // elements of an LDS tile
+  __shared__ __align__(16) bf16 smem[ST * (P + 1) * TS];
+  __shared__ float dbs[W];
+  auto As = [&](int st, int p) { return smem + (st * P + p) * TS; };
+  auto Bs = [&](int st) { return smem + (ST * P + st) * TS; };
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const TileId tl = xcd_tile(false);
-  const int n0 = tl.x * kTile, k0 = tl.y * kTile;
+  const TileId tl = panel_tile();
+  const int n0 = tl.x * W, k0 = tl.y * W;
   const int64_t m0 = (int64_t)tl.z * a.chunk, m1 = min(a.rows, m0 + a.chunk);
-  // dy: rows ar, ar + 16 of a step, columns an .. an + 7; codes: row br,
-  // columns bk .. bk + 15
-  const int ar = tid >> 4, an = (tid & 15) * 8;
-  const int br = tid >> 3, bk = (tid & 7) * 16;
-  const int64_t nleft = a.n - (n0 + an);
-  const bool kin = k0 + bk < a.q.pitch;
-  Raw8<T> ra[2];
-  uint4 rb;
-  uint32_t re;
-  auto gload = [&](int64_t m) {
+  const int steps = (int)((m1 - m0 + kStep - 1) / kStep);
+  // Columns past the matrix are read from its first ones: what they give is
+  // never stored. A vector that straddles the last column reads into the
+  // next row; only the last row of all has none.
+  const int ar = tid / LA, ac = n0 + (tid % LA) * 8;
+  const int br = tid / LB, bc = k0 + (tid % LB) * 16;
+  const int al = ac < a.n ? ac : 0, bl = bc < a.q.pitch ? bc : 0;
+  const int64_t fast = min(m1, a.rows - 1) - kStep;  // steps up to this row read whole vectors
+  struct Slot {
+    Raw8<T> a[NA];
+    uint4 q[NQ];
+    uint32_t e[NQ];
+  } slot[ST];
+  auto gload = [&](Slot &s, int step) {
+    const int64_t m = m0 + (int64_t)step * kStep;
+    const T *pa = (const T *)a.dy.p + m * a.dy.ld;
+    const int8_t *pq = a.q.q + m * a.q.pitch;
+    const uint8_t *pe = a.q.e + m * (a.q.pitch / kGroup);
+    if (m <= fast) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t r = m + ar + 16 * i;
-      ra[i] = load8((const T *)a.dy.p + r * a.dy.ld + n0 + an, r < m1 ? nleft : 0);
-    }
-    const int64_t r = m + br;
-    rb = make_uint4(0, 0, 0, 0);
-    re = 7;
-    if (r < m1 && kin) {
-      rb = *(const uint4 *)(a.q.q + r * a.q.pitch + k0 + bk);
-      re = a.q.e[r * (a.q.pitch / kGroup) + (k0 + bk) / kGroup];
-    }
-  };
-  float dbv[8];
+      for (int i = 0; i < NA; ++i) s.a[i] = load8(pa + (int64_t)(ar + RA * i) * a.dy.ld + al, 8);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) dbv[i] = 0.f;
-  auto store = [&](int st) {
+      for (int i = 0; i < NQ; ++i) {
+        const int64_t r = br + RB * i;
+        s.q[i] = *(const uint4 *)(pq + r * a.q.pitch + bl);
+        s.e[i] = pe[r * (a.q.pitch / kGroup) + bl / kGroup];
+      }
+    } else {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      float v[8];
-      ra[i].get(v);
+      for (int i = 0; i < NA; ++i) {
+        const int64_t r = ar + RA * i;
+        s.a[i] = load8(pa + r * a.dy.ld + al, m + r < m1 ? a.n - al : 0);
+      }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) dbv[e] += v[e];
-      const int at = M::off(ar + 16 * i, an);
-      if constexpr (P == 1) {
-        *(uint4 *)&As[st][0][at] = make_uint4(ra[i].w[0], ra[i].w[1], ra[i].w[2], ra[i].w[3]);
-      } else {
-        float c[8][3];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) cut3(v[e], c[e]);
-#pragma unroll
-        for (int p = 0; p < P; ++p)
-          *(uint4 *)&As[st][p][at] =
-              make_uint4(bf_pair(c[0][p], c[1][p]), bf_pair(c[2][p], c[3][p]),
-                         bf_pair(c[4][p], c[5][p]), bf_pair(c[6][p], c[7][p]));
+      for (int i = 0; i < NQ; ++i) {
+        const int64_t r = br + RB * i;
+        s.q[i] = make_uint4(0, 0, 0, 0);
+        s.e[i] = 7;
+        if (m + r < m1) {
+          s.q[i] = *(const uint4 *)(pq + r * a.q.pitch + bl);
+          s.e[i] = pe[r * (a.q.pitch / kGroup) + bl / kGroup];
+        }
       }
     }
-    float q[16];
-    const float s = step_of(re);
-    decode4(rb.x, s, q), decode4(rb.y, s, q + 4), decode4(rb.z, s, q + 8), decode4(rb.w, s, q + 12);
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      *(uint4 *)&Bs[st][M::off(br, bk + 8 * h)] =
-          make_uint4(bf_pair(q[8 * h], q[8 * h + 1]), bf_pair(q[8 * h + 2], q[8 * h + 3]),
-                     bf_pair(q[8 * h + 4], q[8 * h + 5]), bf_pair(q[8 * h + 6], q[8 * h + 7]));
   };
-  f32x16 acc[2][2];
+  auto put_dy = [&](const Slot &s, int st) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < NA; ++i) {
+      const int at = M::off(ar + RA * i, (tid % LA) * 8);
+      if constexpr (P == 1) {
+        *(uint4 *)(As(st, 0) + at) =
+            make_uint4(s.a[i].w[0], s.a[i].w[1], s.a[i].w[2], s.a[i].w[3]);
+      } else {
+        float v[8], c[P][8];
+        s.a[i].get(v);
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+        for (int e = 0; e < 8; ++e) {
+          float t[3];
+          cut3(v[e], t);
+#pragma unroll
+          for (int p = 0; p < P; ++p) c[p][e] = t[p];
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p) *(uint4 *)(As(st, p) + at) = bf_vec(c[p]);
+      }
+    }
+  };
+  auto put_q = [&](const Slot &s, int st) {
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const float step = step_of(s.e[i]);
+      const uint32_t w[4] = {s.q[i].x, s.q[i].y, s.q[i].z, s.q[i].w};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float v[8];
+        decode4(w[2 * h], step, v), decode4(w[2 * h + 1], step, v + 4);
+        *(uint4 *)(Bs(st) + M::off(br + RB * i, (tid % LB) * 16 + 8 * h)) = bf_vec(v);
+      }
+    }
+  };
+
+  f32x16 acc[NB][NB];
+#pragma unroll
+  for (int i = 0; i < NB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
-  const int wn = (wave & 1) * 64, wk = (wave >> 1) * 64;
-  if (m0 < m1) {
-    gload(m0);
-    store(0);
-  }
-  __syncthreads();
-  int st = 0;
-  for (int64_t m = m0; m < m1; m += kStep) {
-    const bool more = m + kStep < m1;
-    if (more) gload(m + kStep);
-    bf16x8 b[2][2];
+  const int wn = (wave & 1) * (W / 2), wk = (wave >> 1) * (W / 2);
+  // fragments of the unit being multiplied and of the next one; b by slice
+  bf16x8 fa[2][NB], fb[2][NB];
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+  for (int i = 0; i < NB; ++i)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) b[j][s] = ld_tr8<kTile, 2>(Bs[st], wk + 32 * j, s, lane);
+    for (int e = 0; e < 8; ++e) fa[1][i][e] = fb[1][i][e] = (__bf16)0.f;
+  // db: the sums of this wave's fragments of dy, slice 0 or 1 of every step
+  // by the side of k it works on (two waves hold the same dy)
+  const bool want_db = tl.y == 0 || (a.shift && !a.part);
+  float dbv[NB];
 #pragma unroll
-    for (int p = P - 1; p >= 0; --p)
+  for (int i = 0; i < NB; ++i) dbv[i] = 0.f;
+  auto read = [&](int st, auto u) {
+    constexpr int u_ = decltype(u)::value, s = u_ / P, p = u_ % P;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < NB; ++i) fa[u_ & 1][i] = ld_tr8<W, 2>(As(st, p), wn + 32 * i, s, lane);
+    if constexpr (p == 0) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const bf16x8 f = ld_tr8<kTile, 2>(As[st][p], wn + 32 * i, s, lane);
+      for (int j = 0; j < NB; ++j) fb[s][j] = ld_tr8<W, 2>(Bs(st), wk + 32 * j, s, lane);
+    }
+  };
+  auto mma = [&](auto u) {
+    constexpr int u_ = decltype(u)::value, s = u_ / P;
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, b[j][s], acc[i][j], 0, 0, 0);
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[u_ & 1][i], fb[s][j], acc[i][j],
+                                                            0, 0, 0);
+    if (want_db && (wave >> 1) == s) {
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dbv[i] += (float)fa[u_ & 1][i][e];
+    }
+  };
+  using std::integral_constant;
+  // Step t (tile t is in LDS buffer t % ST): units are read one ahead of
+  // their MFMAs; the tile of step t + 1 is written; loads of step t + 1 + ST
+  // take its slot.
+  auto step = [&](auto sc, int t) {
+    constexpr int st = decltype(sc)::value, nx = (st + 1) % ST;
+    const bool more = t + 1 < steps;
+    auto unit = [&](auto u) {
+      constexpr int u_ = decltype(u)::value;
+      read(st, u);
+      mma(integral_constant<int, (u_ + U - 1) % U>());
+      if (more) {
+        if constexpr (u_ == 0) put_dy(slot[nx], nx);
+        if constexpr (u_ == U / 2) {
+          put_q(slot[nx], nx);
+          if (t + 1 + ST < steps) gload(slot[nx], t + 1 + ST);
         }
-    if (more) store(st ^ 1);
+      }
+    };
+    unit(integral_constant<int, 0>());
+    unit(integral_constant<int, 1>());
+    if constexpr (U == 6) {
+      unit(integral_constant<int, 2>());
+      unit(integral_constant<int, 3>());
+      unit(integral_constant<int, 4>());
+      unit(integral_constant<int, 5>());
+    }
     __syncthreads();
-    st ^= 1;
-  }
-  // db of the tile's columns: the 16 row slots added in order
-  float *slots = (float *)&As[0][0][0];  // [16][128]
+  };
+  if (steps > 0) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) slots[ar * kTile + an + e] = dbv[e];
+    for (int i = 0; i < ST; ++i)
+      if (i < steps) gload(slot[i], i);
+    put_dy(slot[0], 0);
+    put_q(slot[0], 0);
+    if (ST < steps) gload(slot[0], ST);
+    __syncthreads();
+    int t = 0;
+    for (; t + ST <= steps; t += ST) {
+      step(integral_constant<int, 0>(), t);
+      step(integral_constant<int, 1>(), t + 1);
+      if constexpr (ST == 3) step(integral_constant<int, 2>(), t + 2);
+    }
+    if (t < steps) step(integral_constant<int, 0>(), t);
+    if (ST == 3 && t + 1 < steps) step(integral_constant<int, 1>(), t + 1);
+    mma(integral_constant<int, U - 1>());
+  }
+  // db of the tile's columns: halves of a fragment, then the two slices
+  float *slots = (float *)smem;  // [2][W]
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    const float s = dbv[i] + __shfl_xor(dbv[i], 32);
+    if (lane < 32) slots[(wave >> 1) * W + wn + 32 * i + lane] = s;
+  }
   __syncthreads();
-  if (tid < kTile) {
-    float s = 0.f;
-    for (int r = 0; r < 16; ++r) s += slots[r * kTile + tid];
+  if (tid < W) {
+    const float s = slots[tid] + slots[W + tid];
     dbs[tid] = s;
     const int nn = n0 + tid;
     if (tl.y == 0 && nn < a.n) {
@@ -165,13 +275,13 @@ __global__ __launch_bounds__(256, 2) void wgrad8_kernel(WgArgs a) {
   __syncthreads();
   float *out = a.part ? a.part + (int64_t)tl.z * a.n * a.k : a.dw;
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
+  for (int j = 0; j < NB; ++j) {
     const int kk = k0 + wk + 32 * j + (lane & 31);
     if (kk >= a.k) continue;
     const float sc = a.scale && !a.part ? a.scale[kk] : 1.f;
     const float sh = a.shift && !a.part ? a.shift[kk] : 0.f;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < NB; ++i)
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         const int nl = wn + 32 * i + acc_row(v, lane);
@@ -234,16 +344,17 @@ __global__ __launch_bounds__(256) void wgrad8_join_kernel(WgArgs a, int splits) 
   if (k == 0 && a.db) a.db[n] = a.accumulate ? a.db[n] + d : d;
 }
 
-// Rows per split: two workgroups a CU, at least 256 rows each.
+// Tile width and rows per split.
 struct Split {
-  int splits;
+  int tile, splits;
   int64_t chunk;
 };
 Split split_of(int64_t rows, int64_t n, int64_t k) {
-  const int64_t tiles = ((n + kTile - 1) / kTile) * ((k + kTile - 1) / kTile);
-  int64_t s = std::max<int64_t>(1, 512 / tiles);
-  s = std::min(s, std::max<int64_t>(1, rows / 256));
   Split r;
+  auto tiles = [&](int w) { return ((n + w - 1) / w) * ((k + w - 1) / w); };
+  r.tile = n > 128 && k > 128 && tiles(256) * std::max<int64_t>(1, rows / 1024) >= 256 ? 256 : 128;
+  int64_t s = std::max<int64_t>(1, (r.tile == 256 ? 256 : 512) / tiles(r.tile));
+  s = std::min(s, std::max<int64_t>(1, rows / 256));
   r.chunk = ((rows + s - 1) / s + kStep - 1) / kStep * kStep;
   if (r.chunk < kStep) r.chunk = kStep;
   r.splits = (int)std::max<int64_t>(1, (rows + r.chunk - 1) / r.chunk);
@@ -308,12 +419,18 @@ extern "C" int lrcnn_linear_wgrad(int64_t rows, int64_t n_in, int64_t n_out, int
     a.part = (float *)workspace;
     a.dbpart = (float *)((char *)workspace + a256((size_t)sp.splits * n_out * n_in * 4));
   }
-  const dim3 grid((unsigned)((n_out + kTile - 1) / kTile), (unsigned)((n_in + kTile - 1) / kTile),
-                  (unsigned)sp.splits);
-  if (grid.y > 65535) return lrcnn_fail(LRCNN_ESHAPE, "too many input features");
+  const dim3 grid((unsigned)((n_out + sp.tile - 1) / sp.tile),
+                  (unsigned)((n_in + sp.tile - 1) / sp.tile), (unsigned)sp.splits);
+  if (grid.y > 65535 || (int64_t)grid.x * grid.y * grid.z > INT32_MAX)
+    return lrcnn_fail(LRCNN_ESHAPE, "too many features");
   hipStream_t s = (hipStream_t)stream;
-  if (dtype == LRCNN_BF16) wgrad8_kernel<bf16><<<grid, 256, 0, s>>>(a);
-  else wgrad8_kernel<float><<<grid, 256, 0, s>>>(a);
+  auto run = [&](auto *t) {
+    using T = std::remove_pointer_t<decltype(t)>;
+    if (sp.tile == 256) wgrad8_kernel<T, 256><<<grid, 256, 0, s>>>(a);
+    else wgrad8_kernel<T, 128><<<grid, 256, 0, s>>>(a);
+  };
+  if (dtype == LRCNN_BF16) run((bf16 *)nullptr);
+  else run((float *)nullptr);
   if (sp.splits > 1) {
     const int64_t nk = n_out * n_in;
     if (n_in % 4 == 0 && ((uintptr_t)workspace & 15) == 0)
