@@ -21,12 +21,14 @@ namespace lrcnn {
 namespace act8 {
 namespace {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+constexpr int64_t kMaxFeatures = 1 << 24;  // 31 rows within 32-bit offsets
 constexpr int kStep = 32;  // rows of dy and of the checkpoint per step
 
 struct WgArgs {
   int64_t rows;
   int n, k;             // outputs, inputs
-  int64_t chunk;        // rows per split, a multiple of kStep
+  int splits;           // split z takes the steps z, z + splits, ...
   Mat dy;
   Ckpt q;
   const float *scale, *shift;
@@ -38,13 +40,48 @@ struct WgArgs {
 // hi + mid + lo == v (hi alone where v is not finite)
 __device__ __forceinline__ void cut3(float v, float (&p)[3]) {
   p[0] = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
-  const float r = (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u ? 0.f : v - p[0];
+  float r = v - p[0];
+  r = r == r ? r : 0.f;
   p[1] = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
   p[2] = r - p[1];
 }
 __device__ __forceinline__ uint4 bf_vec(const float *v) {
   return make_uint4(bf_pair(v[0], v[1]), bf_pair(v[2], v[3]), bf_pair(v[4], v[5]),
                     bf_pair(v[6], v[7]));
+}
+
+// Eight columns moved down by d < 8, per lane: a vector read d columns early
+// so as to end with the last column.
+__device__ __forceinline__ Raw8<bf16> moved_down(const Raw8<bf16> &r, int d) {
+  const bool b4 = d & 4, b2 = d & 2, b1 = d & 1;
+  const uint32_t x0 = b4 ? r.w[2] : r.w[0], x1 = b4 ? r.w[3] : r.w[1], x2 = r.w[2], x3 = r.w[3];
+  const uint32_t y0 = b2 ? x1 : x0, y1 = b2 ? x2 : x1, y2 = b2 ? x3 : x2;
+  Raw8<bf16> o;
+  o.w[0] = b1 ? __builtin_amdgcn_alignbit(y1, y0, 16) : y0;
+  o.w[1] = b1 ? __builtin_amdgcn_alignbit(y2, y1, 16) : y1;
+  o.w[2] = b1 ? __builtin_amdgcn_alignbit(x3, y2, 16) : y2;
+  o.w[3] = b1 ? x3 >> 16 : x3;
+  return o;
+}
+__device__ __forceinline__ Raw8<float> moved_down(const Raw8<float> &r, int d) {
+  const bool b4 = d & 4, b2 = d & 2, b1 = d & 1;
+  const float x0 = b4 ? r.b[0] : r.a[0], x1 = b4 ? r.b[1] : r.a[1];
+  const float x2 = b4 ? r.b[2] : r.a[2], x3 = b4 ? r.b[3] : r.a[3];
+  const float y0 = b2 ? x2 : x0, y1 = b2 ? x3 : x1, y2 = b2 ? r.b[0] : x2;
+  const float y3 = b2 ? r.b[1] : x3, y4 = b2 ? r.b[2] : r.b[0], y5 = b2 ? r.b[3] : r.b[1];
+  Raw8<float> o;
+  o.a = (f32x4_a4){b1 ? y1 : y0, b1 ? y2 : y1, b1 ? y3 : y2, b1 ? y4 : y3};
+  o.b = (f32x4_a4){b1 ? y5 : y4, b1 ? r.b[2] : y5, b1 ? r.b[3] : r.b[2], r.b[3]};
+  return o;
+}
+
+// f(0), f(1), ... f(N - 1), the index a constant
+template <int B, int E, typename F>
+__device__ __forceinline__ void each(F &&f) {
+  if constexpr (B < E) {
+    f(std::integral_constant<int, B>());
+    each<B + 1, E>(f);
+  }
 }
 
 // Tiles run through a panel of eight tiles of n before the next k, so that
@@ -59,13 +96,29 @@ __device__ __forceinline__ TileId panel_tile() {
   return t;
 }
 
+constexpr int least(int a, int b) { return a < b ? a : b; }
+
+// How a thread reads its eight columns of dy.
+enum Cols {
+  COLS_WHOLE,  // n a multiple of 8: a vector has all its columns or none
+  COLS_SHIFT,  // the vector with the last column is read earlier and moved
+  COLS_EACH    // n < 8: one by one
+};
+
 // A W x W tile of S by four waves of W/2 x W/2. Both operands go through
 // registers into k-major LDS tiles (the codes as bfloat16, dy as it is or in
 // three pieces), and to the matrix cores by transposing reads. A step's loads
-// are issued RS steps before its tile is written to LDS, the tile is written
+// are issued ST steps before its tile is written to LDS, the tile is written
 // one step before it is multiplied, and a unit's fragments (16 rows; one
 // piece of dy) are read one unit before their MFMAs.
-template <typename T, int W>
+//
+// There is one kind of step in the loop. Rows left over from whole steps are
+// taken first, as the matrix' last 32 rows of which those that a whole step
+// has count as zeros, and the steps that fill up the last round of ST multiply
+// by zero; so the code that runs once is short (a second, guarded kind of step
+// cost 40 us a launch in instruction fetches alone). Columns past the matrix
+// are read from its first ones: what they give is never stored.
+template <typename T, int W, int COLS>
 __global__ __launch_bounds__(256, W == 256 ? 1 : 2) void wgrad8_kernel(WgArgs a) {
   constexpr int P = std::is_same<T, float>::value ? 3 : 1;  // pieces of dy
   constexpr int ST = P == 1 ? 3 : 2;                         // LDS tiles and load slots
@@ -74,94 +127,147 @@ __global__ __launch_bounds__(256, W == 256 ? 1 : 2) void wgrad8_kernel(WgArgs a)
   constexpr int LA = W / 8, RA = 256 / LA, NA = kStep / RA;  // dy: lanes, rows, passes
   constexpr int LB = W / 16, RB = 256 / LB, NQ = kStep / RB; // codes
   using M = KM<bf16, W>;
-  constexpr int TS = kStep * W;  // elements of an LDS tile
-  __shared__ __align__(16) bf16 smem[ST * (P + 1) * TS];
+  constexpr int TB = kStep * W * 2;  // bytes of an LDS tile
+  constexpr int EP = W / 2 + 8;      // float pitch of the epilogue's 32-row strips
+  constexpr int LDS = ST * (P + 1) * TB > 512 * EP ? ST * (P + 1) * TB : 512 * EP;
+  __shared__ __align__(16) char smem[LDS];
   __shared__ float dbs[W];
-  auto As = [&](int st, int p) { return smem + (st * P + p) * TS; };
-  auto Bs = [&](int st) { return smem + (ST * P + st) * TS; };
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63,
+            wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const TileId tl = panel_tile();
   const int n0 = tl.x * W, k0 = tl.y * W;
-  const int64_t m0 = (int64_t)tl.z * a.chunk, m1 = min(a.rows, m0 + a.chunk);
-  const int steps = (int)((m1 - m0 + kStep - 1) / kStep);
-  // Columns past the matrix are read from its first ones: what they give is
-  // never stored. A vector that straddles the last column reads into the
-  // next row; only the last row of all has none.
+  // This split's steps: every splits-th run of kStep rows, so that the
+  // workgroups together read one window of rows that moves on
+  const int64_t stride = (int64_t)a.splits * kStep, first = (int64_t)tl.z * kStep;
+  const int steps = first < a.rows ? (int)((a.rows - first + stride - 1) / stride) : 0;
+  const int some = (int)min(a.rows, (int64_t)kStep);  // rows a step can read
   const int ar = tid / LA, ac = n0 + (tid % LA) * 8;
   const int br = tid / LB, bc = k0 + (tid % LB) * 16;
-  const int al = ac < a.n ? ac : 0, bl = bc < a.q.pitch ? bc : 0;
-  const int64_t fast = min(m1, a.rows - 1) - kStep;  // steps up to this row read whole vectors
+  int al = ac < a.n ? ac : 0, down = 0;
+  if (COLS == COLS_SHIFT && ac < a.n && ac + 8 > a.n) al = a.n - 8, down = ac + 8 - a.n;
+  const int bl = bc < a.q.pitch ? bc : 0;
+  const int64_t pe_ld = a.q.pitch / kGroup;
+  uint32_t oa[NA], oq[NQ], oe[NQ];  // bytes from a step's first row
+#pragma unroll
+  for (int i = 0; i < NA; ++i)
+    oa[i] = (uint32_t)((min(ar + RA * i, some - 1) * a.dy.ld + al) * sizeof(T));
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const int r = min(br + RB * i, some - 1);
+    oq[i] = (uint32_t)(r * a.q.pitch + bl);
+    oe[i] = (uint32_t)(r * pe_ld + bl / kGroup);
+  }
   struct Slot {
     Raw8<T> a[NA];
     uint4 q[NQ];
     uint32_t e[NQ];
+    float live;  // 1, or 0 in a step that only fills up the last round
   } slot[ST];
-  auto gload = [&](Slot &s, int step) {
-    const int64_t m = m0 + (int64_t)step * kStep;
-    const T *pa = (const T *)a.dy.p + m * a.dy.ld;
-    const int8_t *pq = a.q.q + m * a.q.pitch;
-    const uint8_t *pe = a.q.e + m * (a.q.pitch / kGroup);
-    if (m <= fast) {
+  // The step to load: its number and its first row in the three arrays
+  const int64_t ia = stride * a.dy.ld * (int64_t)sizeof(T), iq = stride * a.q.pitch,
+                ie = stride * pe_ld;
+  int nt = 0;
+  float live = 1.f;
+  const char *ga, *gq, *ge;
+  auto place = [&](int64_t m) {
+    ga = a.dy.p + m * a.dy.ld * (int64_t)sizeof(T);
+    gq = (const char *)a.q.q + m * a.q.pitch;
+    ge = (const char *)a.q.e + m * pe_ld;
+  };
+  // this split's last step is not whole: it comes first, `zero` rows early
+  const int64_t over = first + steps * stride - stride + kStep - a.rows;
+  const bool odd = over > 0;
+  const int zero = odd && a.rows >= kStep ? (int)over : 0;
+  place(odd ? max(a.rows - kStep, (int64_t)0) : first);
+  // (past the end the last step again. Scalar bases that the compiler may not
+  // fold into one address per lane and load.)
+  auto advance = [&]() {
+    ++nt;
+    const bool on = nt < steps;
+    ga += on ? ia : 0, gq += on ? iq : 0, ge += on ? ie : 0;
+    live = on ? 1.f : 0.f;
+    asm volatile("" : "+s"(ga), "+s"(gq), "+s"(ge));
+  };
+  typedef __attribute__((address_space(1))) const char g_char;
+  auto gload_dy = [&](Slot &s, int i) {
+    uint32_t o = oa[i];
+    asm volatile("" : "+v"(o));
+    g_char *p = (g_char *)ga + o;
+    if constexpr (COLS == COLS_EACH) {
+      float v[8];
 #pragma unroll
-      for (int i = 0; i < NA; ++i) s.a[i] = load8(pa + (int64_t)(ar + RA * i) * a.dy.ld + al, 8);
+      for (int e = 0; e < 8; ++e)
+        v[e] = to_f(((__attribute__((address_space(1))) const T *)p)[min(e, a.n - 1)]);
+      if constexpr (P == 1) {
 #pragma unroll
-      for (int i = 0; i < NQ; ++i) {
-        const int64_t r = br + RB * i;
-        s.q[i] = *(const uint4 *)(pq + r * a.q.pitch + bl);
-        s.e[i] = pe[r * (a.q.pitch / kGroup) + bl / kGroup];
+        for (int e = 0; e < 4; ++e) s.a[i].w[e] = bf_pair(v[2 * e], v[2 * e + 1]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s.a[i].a[e] = v[e], s.a[i].b[e] = v[4 + e];
+      }
+    } else if constexpr (P == 1) {
+      s.a[i].w = *(__attribute__((address_space(1))) const u32x4_a2 *)p;
+    } else {
+      s.a[i].a = *(__attribute__((address_space(1))) const f32x4_a4 *)p;
+      s.a[i].b = *(__attribute__((address_space(1))) const f32x4_a4 *)(p + 16);
+    }
+  };
+  auto gload_q = [&](Slot &s, int i) {
+    uint32_t o = oq[i], oe_ = oe[i];
+    asm volatile("" : "+v"(o), "+v"(oe_));
+    const u32x4 v = *(__attribute__((address_space(1))) const u32x4 *)((g_char *)gq + o);
+    s.q[i] = make_uint4(v.x, v.y, v.z, v.w);
+    s.e[i] = *(__attribute__((address_space(1))) const uint8_t *)((g_char *)ge + oe_);
+  };
+  // LDS bytes of this thread's writes; passes are whole swizzle periods apart
+  typedef __attribute__((address_space(3))) char lds_char;
+  lds_char *lds = (lds_char *)smem;
+  const int wa = 2 * M::off(ar, (tid % LA) * 8);
+  const int wq = ST * P * TB + 2 * M::off(br, (tid % LB) * 16);
+  auto put = [&](int at, uint4 v) {
+    typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+    *(lds_u32x4 *)(lds + at) = (u32x4){v.x, v.y, v.z, v.w};
+  };
+  // One of the eight columns of pass i of dy: with one piece the last one
+  // writes them all; with three each is cut, and the last one writes.
+  // FIRST: rows that do not count become zeros.
+  uint32_t cut[P][4];
+  float even[P];
+  auto put_dy = [&](const Slot &s, int st, auto k, auto first_) {
+    constexpr int i = decltype(k)::value / 8, e = decltype(k)::value % 8;
+    const int at = wa + st * P * TB + 2 * RA * W * i;
+    const int r = ar + RA * i;
+    const bool in = !decltype(first_)::value || (r >= zero && r < some);
+    if constexpr (P == 1) {
+      if constexpr (e == 7) {
+        const Raw8<T> x = COLS == COLS_SHIFT ? moved_down(s.a[i], down) : s.a[i];
+        put(at, make_uint4(in ? x.w[0] : 0, in ? x.w[1] : 0, in ? x.w[2] : 0, in ? x.w[3] : 0));
       }
     } else {
+      const Raw8<T> x = COLS == COLS_SHIFT ? moved_down(s.a[i], down) : s.a[i];
+      float t[3];
+      cut3(in ? e < 4 ? x.a[e & 3] : x.b[e & 3] : 0.f, t);
 #pragma unroll
-      for (int i = 0; i < NA; ++i) {
-        const int64_t r = ar + RA * i;
-        s.a[i] = load8(pa + r * a.dy.ld + al, m + r < m1 ? a.n - al : 0);
-      }
-#pragma unroll
-      for (int i = 0; i < NQ; ++i) {
-        const int64_t r = br + RB * i;
-        s.q[i] = make_uint4(0, 0, 0, 0);
-        s.e[i] = 7;
-        if (m + r < m1) {
-          s.q[i] = *(const uint4 *)(pq + r * a.q.pitch + bl);
-          s.e[i] = pe[r * (a.q.pitch / kGroup) + bl / kGroup];
-        }
+      for (int p = 0; p < P; ++p) {
+        if constexpr (e % 2 == 0) even[p] = t[p];
+        else cut[p][e / 2] = bf_pair(even[p], t[p]);
+        if constexpr (e == 7)
+          put(at + p * TB, make_uint4(cut[p][0], cut[p][1], cut[p][2], cut[p][3]));
       }
     }
   };
-  auto put_dy = [&](const Slot &s, int st) {
-#pragma unroll
-    for (int i = 0; i < NA; ++i) {
-      const int at = M::off(ar + RA * i, (tid % LA) * 8);
-      if constexpr (P == 1) {
-        *(uint4 *)(As(st, 0) + at) =
-            make_uint4(s.a[i].w[0], s.a[i].w[1], s.a[i].w[2], s.a[i].w[3]);
-      } else {
-        float v[8], c[P][8];
-        s.a[i].get(v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          float t[3];
-          cut3(v[e], t);
-#pragma unroll
-          for (int p = 0; p < P; ++p) c[p][e] = t[p];
-        }
-#pragma unroll
-        for (int p = 0; p < P; ++p) *(uint4 *)(As(st, p) + at) = bf_vec(c[p]);
-      }
-    }
-  };
-  auto put_q = [&](const Slot &s, int st) {
-#pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-      const float step = step_of(s.e[i]);
-      const uint32_t w[4] = {s.q[i].x, s.q[i].y, s.q[i].z, s.q[i].w};
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float v[8];
-        decode4(w[2 * h], step, v), decode4(w[2 * h + 1], step, v + 4);
-        *(uint4 *)(Bs(st) + M::off(br + RB * i, (tid % LB) * 16 + 8 * h)) = bf_vec(v);
-      }
-    }
+  // One of the sixteen codes of pass i
+  float qstep, qeven;
+  uint32_t qw[4];
+  auto put_q = [&](const Slot &s, int st, auto k) {
+    constexpr int i = decltype(k)::value / 16, c = decltype(k)::value % 16;
+    if constexpr (c == 0) qstep = step_of(s.e[i]) * s.live;
+    const uint32_t w = c < 4 ? s.q[i].x : c < 8 ? s.q[i].y : c < 12 ? s.q[i].z : s.q[i].w;
+    const float v = (float)(int8_t)(w >> (8 * (c % 4))) * qstep;
+    if constexpr (c % 2 == 0) qeven = v;
+    else qw[c / 2 % 4] = bf_pair(qeven, v);
+    if constexpr (c % 8 == 7)
+      put(wq + st * TB + 2 * RB * W * i + 2 * (c - 7), make_uint4(qw[0], qw[1], qw[2], qw[3]));
   };
 
   f32x16 acc[NB][NB];
@@ -172,89 +278,141 @@ __global__ __launch_bounds__(256, W == 256 ? 1 : 2) void wgrad8_kernel(WgArgs a)
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
   const int wn = (wave & 1) * (W / 2), wk = (wave >> 1) * (W / 2);
-  // fragments of the unit being multiplied and of the next one; b by slice
-  bf16x8 fa[2][NB], fb[2][NB];
+  // fragments of the unit being multiplied and of the next one, as the two
+  // reads that fetch them; b by slice
+  bf16x4 fa[2][NB][2], fb[2][NB][2];
 #pragma unroll
-  for (int i = 0; i < NB; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) fa[1][i][e] = fb[1][i][e] = (__bf16)0.f;
-  // db: the sums of this wave's fragments of dy, slice 0 or 1 of every step
-  // by the side of k it works on (two waves hold the same dy)
-  const bool want_db = tl.y == 0 || (a.shift && !a.part);
+  for (int i = 0; i < 2 * NB; ++i)
+    fa[1][i / 2][i % 2] = fb[1][i / 2][i % 2] = (bf16x4){(__bf16)0.f, (__bf16)0.f, (__bf16)0.f, (__bf16)0.f};
   float dbv[NB];
 #pragma unroll
   for (int i = 0; i < NB; ++i) dbv[i] = 0.f;
-  auto read = [&](int st, auto u) {
-    constexpr int u_ = decltype(u)::value, s = u_ / P, p = u_ % P;
+  // A transposing read hands lane 16 G + 4 r + c of a wave the elements of
+  // column 16 (G & 1) + its own place in the 16 lanes, of the K rows
+  // 16 (G >> 1) + 8 s + [0, 4); a second one, four rows on, the next four.
+  // The row's swizzle depends on r alone, so blocks of 32 columns are an
+  // address each, and everything else is a constant.
+  int pa_[NB], pb_[NB];
+  {
+    const int G = lane >> 4, r = (lane >> 2) & 3, c = 16 * (G & 1) + 4 * (lane & 3);
 #pragma unroll
-    for (int i = 0; i < NB; ++i) fa[u_ & 1][i] = ld_tr8<W, 2>(As(st, p), wn + 32 * i, s, lane);
-    if constexpr (p == 0) {
-#pragma unroll
-      for (int j = 0; j < NB; ++j) fb[s][j] = ld_tr8<W, 2>(Bs(st), wk + 32 * j, s, lane);
+    for (int i = 0; i < NB; ++i) {
+      pa_[i] = 2 * M::off(16 * (G >> 1) + r, wn + 32 * i + c);
+      pb_[i] = ST * P * TB + 2 * M::off(16 * (G >> 1) + r, wk + 32 * i + c);
     }
+  }
+  auto read = [&](int at) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4 *)(lds + at));
   };
-  auto mma = [&](auto u) {
-    constexpr int u_ = decltype(u)::value, s = u_ / P;
-#pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-      for (int j = 0; j < NB; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[u_ & 1][i], fb[s][j], acc[i][j],
-                                                            0, 0, 0);
-    if (want_db && (wave >> 1) == s) {
-#pragma unroll
-      for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) dbv[i] += (float)fa[u_ & 1][i][e];
-    }
+  auto whole8 = [&](const bf16x4 (&h)[2]) {
+    return __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
   };
   using std::integral_constant;
-  // Step t (tile t is in LDS buffer t % ST): units are read one ahead of
-  // their MFMAs; the tile of step t + 1 is written; loads of step t + 1 + ST
-  // take its slot.
-  auto step = [&](auto sc, int t) {
-    constexpr int st = decltype(sc)::value, nx = (st + 1) % ST;
-    const bool more = t + 1 < steps;
-    auto unit = [&](auto u) {
-      constexpr int u_ = decltype(u)::value;
-      read(st, u);
-      mma(integral_constant<int, (u_ + U - 1) % U>());
-      if (more) {
-        if constexpr (u_ == 0) put_dy(slot[nx], nx);
-        if constexpr (u_ == U / 2) {
-          put_q(slot[nx], nx);
-          if (t + 1 + ST < steps) gload(slot[nx], t + 1 + ST);
-        }
+  // A step on LDS tile st. Its order is laid down instruction by
+  // instruction: a slot is one MFMA, which holds the matrix pipe for eight
+  // issue slots of the only wave on it, and a share of everything else -- the
+  // LDS reads of the next unit's fragments, the next step's tile written from
+  // its load slot, the loads that take the slot's place. Left to itself the
+  // compiler puts the MFMAs in runs, and the matrix pipe idles between them.
+  // The last slots before the barrier have no LDS access to wait for.
+  // D: the slice whose fragments of dy this wave sums for db (two waves hold
+  // the same dy and take one each), or 2: db is not wanted here.
+  uint32_t one_now = 0x3f803f80u, one_was = 0x3f803f80u;  // bfloat16 ones, or zeros
+  auto step = [&](auto sc, auto d, int t_) {
+    one_was = one_now;
+    one_now = t_ < steps ? 0x3f803f80u : 0u;
+    constexpr int st = decltype(sc)::value, nx = (st + 1) % ST, D = decltype(d)::value;
+    constexpr int MF = NB * NB, S = U * MF, Q = MF / 4;  // slots of a unit, of the step
+    each<0, S>([&](auto slot_) {
+      constexpr int t = decltype(slot_)::value, u = t / MF, m = t % MF;
+      // multiply: the unit before u
+      constexpr int v = (u + U - 1) % U, s = v / P, i = m / NB, j = m % NB;
+      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(whole8(fa[v & 1][i]), whole8(fb[s][j]),
+                                                          acc[i][j], 0, 0, 0);
+      if constexpr (D == s) {
+        const bf16x2 one = __builtin_bit_cast(bf16x2, u ? one_now : one_was);
+        each<4 * NB * m / MF, 4 * NB * (m + 1) / MF>([&](auto x) {
+          constexpr int k = decltype(x)::value, e = k % 4;
+          const bf16x4 h = fa[v & 1][k / 4][e / 2];
+          dbv[k / 4] = __builtin_amdgcn_fdot2_f32_bf16((bf16x2){h[2 * (e % 2)], h[2 * (e % 2) + 1]},
+                                                       one, dbv[k / 4], false);
+        });
       }
-    };
-    unit(integral_constant<int, 0>());
-    unit(integral_constant<int, 1>());
-    if constexpr (U == 6) {
-      unit(integral_constant<int, 2>());
-      unit(integral_constant<int, 3>());
-      unit(integral_constant<int, 4>());
-      unit(integral_constant<int, 5>());
-    }
+      // read: unit u
+      constexpr int su = u / P, p = u % P, R = (p == 0 ? 4 : 2) * NB, L = MF - Q;
+      each<R * least(m, L) / L, R * least(m + 1, L) / L>([&](auto x) {
+        constexpr int k = decltype(x)::value, h = k % 2, f = k / 2 % NB;
+        const int at = 16 * W * su + 8 * W * h;
+        // b first: the first MFMAs of a unit take all of b and a's first
+        if constexpr (p == 0 && k < 2 * NB) fb[su][f][h] = read(pb_[f] + st * TB + at);
+        else fa[u & 1][f][h] = read(pa_[f] + (st * P + p) * TB + at);
+      });
+      // write the next step's tile and load into its slot
+      constexpr int N = S - Q;
+      constexpr int SA = P == 1 ? N / 2 : 2 * N / 3, S0 = P == 1 ? 0 : SA;  // dy until, codes from
+      each<8 * NA * least(t, SA) / SA, 8 * NA * least(t + 1, SA) / SA>([&](auto x) {
+        put_dy(slot[nx], nx, x, std::false_type());
+        if constexpr (decltype(x)::value % 8 == 7) gload_dy(slot[nx], decltype(x)::value / 8);
+      });
+      constexpr int q0 = t < S0 ? 0 : least(t, N) - S0, q1 = t < S0 ? 0 : least(t + 1, N) - S0;
+      each<16 * NQ * q0 / (N - S0), 16 * NQ * q1 / (N - S0)>([&](auto x) {
+        put_q(slot[nx], nx, x);
+        if constexpr (decltype(x)::value % 16 == 15) gload_q(slot[nx], decltype(x)::value / 16);
+      });
+      // the step to load next, once this one's loads are out
+      if constexpr (t == S - 2) {
+        slot[nx].live = live;
+        advance();
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    });
     __syncthreads();
+  };
+  auto all_steps = [&](auto d) {
+    for (int t = 0; t < steps; t += ST) {
+      step(integral_constant<int, 0>(), d, t);
+      step(integral_constant<int, 1>(), d, t + 1);
+      if constexpr (ST == 3) step(integral_constant<int, 2>(), d, t + 2);
+    }
+    // the last unit of the last step
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(whole8(fa[1][i]), whole8(fb[1][j]),
+                                                            acc[i][j], 0, 0, 0);
+      if constexpr (decltype(d)::value == 1) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dbv[i] += one_now ? (float)fa[1][i][e / 4][e % 4] : 0.f;
+      }
+    }
   };
   if (steps > 0) {
 #pragma unroll
-    for (int i = 0; i < ST; ++i)
-      if (i < steps) gload(slot[i], i);
-    put_dy(slot[0], 0);
-    put_q(slot[0], 0);
-    if (ST < steps) gload(slot[0], ST);
-    __syncthreads();
-    int t = 0;
-    for (; t + ST <= steps; t += ST) {
-      step(integral_constant<int, 0>(), t);
-      step(integral_constant<int, 1>(), t + 1);
-      if constexpr (ST == 3) step(integral_constant<int, 2>(), t + 2);
+    for (int t = 0; t <= ST; ++t) {
+      if (t == ST) {
+        each<0, 8 * NA>([&](auto x) { put_dy(slot[0], 0, x, std::true_type()); });
+        each<0, 16 * NQ>([&](auto x) { put_q(slot[0], 0, x); });
+      }
+      Slot &s = slot[t % ST];
+      // (in the order in which the steps take them)
+#pragma unroll
+      for (int i = 0; i < NA; ++i) gload_dy(s, i);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) gload_q(s, i);
+      __builtin_amdgcn_sched_barrier(0);
+      s.live = live;
+      advance();
+      if (t == 0 && odd && steps > 1) place(first);
     }
-    if (t < steps) step(integral_constant<int, 0>(), t);
-    if (ST == 3 && t + 1 < steps) step(integral_constant<int, 1>(), t + 1);
-    mma(integral_constant<int, U - 1>());
+    __syncthreads();
+    const bool want_db = tl.y == 0 || (a.shift && !a.part);
+    if (!want_db) all_steps(integral_constant<int, 2>());
+    else if (wave < 2) all_steps(integral_constant<int, 0>());
+    else all_steps(integral_constant<int, 1>());
   }
+  __syncthreads();
   // db of the tile's columns: halves of a fragment, then the two slices
   float *slots = (float *)smem;  // [2][W]
 #pragma unroll
@@ -265,7 +423,7 @@ __global__ __launch_bounds__(256, W == 256 ? 1 : 2) void wgrad8_kernel(WgArgs a)
   __syncthreads();
   if (tid < W) {
     const float s = slots[tid] + slots[W + tid];
-    dbs[tid] = s;
+    dbs[tid] = a.shift ? s : 0.f;
     const int nn = n0 + tid;
     if (tl.y == 0 && nn < a.n) {
       if (a.part) a.dbpart[(int64_t)tl.z * a.n + nn] = s;
@@ -273,46 +431,76 @@ __global__ __launch_bounds__(256, W == 256 ? 1 : 2) void wgrad8_kernel(WgArgs a)
     }
   }
   __syncthreads();
+  // dW by rows: a wave turns 32 rows of its part at a time in its own LDS
+  // (lane l holds column l & 31 of rows 4 (l >> 5) + constants of a block)
+  constexpr int V = W / 128;
+  float *own = (float *)smem + wave * 32 * EP;
   float *out = a.part ? a.part + (int64_t)tl.z * a.n * a.k : a.dw;
+  const int kk = k0 + wk + V * lane;
+  float sc[V], sh[V];
 #pragma unroll
-  for (int j = 0; j < NB; ++j) {
-    const int kk = k0 + wk + 32 * j + (lane & 31);
-    if (kk >= a.k) continue;
-    const float sc = a.scale && !a.part ? a.scale[kk] : 1.f;
-    const float sh = a.shift && !a.part ? a.shift[kk] : 0.f;
+  for (int c = 0; c < V; ++c) {
+    const bool in = kk + c < a.k && !a.part;
+    sc[c] = in && a.scale ? a.scale[kk + c] : 1.f;
+    sh[c] = in && a.shift ? a.shift[kk + c] : 0.f;
+  }
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
+  for (int i = 0; i < NB; ++i) {
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int nl = wn + 32 * i + acc_row(v, lane);
-        if (n0 + nl >= a.n) continue;
-        float *d = out + (int64_t)(n0 + nl) * a.k + kk;
-        float r = acc[i][j][v];
-        if (!a.part) {
-          if (a.scale) r *= sc;
-          if (a.shift) r = fmaf(sh, dbs[nl], r);
-          if (a.accumulate) r += *d;
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) own[acc_row(v, lane) * EP + 32 * j + (lane & 31)] = acc[i][j][v];
+    __builtin_amdgcn_wave_barrier();
+    const int nb = wn + 32 * i, rows = min(32, a.n - n0 - nb);
+    typedef __attribute__((address_space(1))) float g_float;
+    g_float *at = (g_float *)out + (int64_t)(n0 + nb) * a.k + kk;
+#pragma unroll 1
+    for (int r = 0; r < rows; r += 8) {
+      // eight rows on their way at a time
+      float x[8][V], b[8], old[8][V];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        b[e] = dbs[nb + r + e];
+#pragma unroll
+        for (int c = 0; c < V; ++c) {
+          x[e][c] = own[(r + e) * EP + V * lane + c];
+          old[e][c] = 0.f;
         }
-        *d = r;
       }
+      if (a.accumulate && !a.part) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int c = 0; c < V; ++c)
+            if (r + e < rows && kk + c < a.k) old[e][c] = at[(int64_t)(r + e) * a.k + c];
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int c = 0; c < V; ++c)
+          if (r + e < rows && kk + c < a.k)
+            at[(int64_t)(r + e) * a.k + c] = fmaf(sh[c], b[e], x[e][c] * sc[c]) + old[e][c];
+    }
   }
 }
 
-// dW and db from the splits' sums, added in a fixed order: eight groups of 32
-// threads take the splits z = g, g + 8, ... of 32 vectors of V columns, then
-// the groups' sums are added in order.
-template <int V>
+// dW and db from the splits' sums, added in a fixed order: G groups of 256 / G
+// threads take the splits z = g, g + G, ... of as many vectors of V columns,
+// then the groups' sums are added in order.
+template <int V, int G>
 __global__ __launch_bounds__(256) void wgrad8_join_kernel(WgArgs a, int splits) {
-  __shared__ float red[8][32][V + 1];
-  const int g = threadIdx.x >> 5, e = threadIdx.x & 31;
-  const int64_t nk = (int64_t)a.n * a.k, i = ((int64_t)blockIdx.x * 32 + e) * V;
+  constexpr int E = 256 / G;
+  __shared__ float red[G][E][V + 1];
+  const int g = threadIdx.x / E, e = threadIdx.x % E;
+  const int64_t nk = (int64_t)a.n * a.k, i = ((int64_t)blockIdx.x * E + e) * V;
   float s[V], d = 0.f;
   const int n = i < nk ? (int)(i / a.k) : 0, k = (int)(i - (int64_t)n * a.k);
 #pragma unroll
   for (int c = 0; c < V; ++c) s[c] = 0.f;
   if (i < nk) {
 #pragma unroll 4
-    for (int z = g; z < splits; z += 8) {
+    for (int z = g; z < splits; z += G) {
       const float *p = a.part + z * nk + i;
       if constexpr (V == 4) {
         const float4 q = *(const float4 *)p;
@@ -323,45 +511,53 @@ __global__ __launch_bounds__(256) void wgrad8_join_kernel(WgArgs a, int splits) 
       d += a.dbpart[(int64_t)z * a.n + n];
     }
   }
+  if constexpr (G > 1) {
 #pragma unroll
-  for (int c = 0; c < V; ++c) red[g][e][c] = s[c];
-  red[g][e][V] = d;
-  __syncthreads();
-  if (g || i >= nk) return;
+    for (int c = 0; c < V; ++c) red[g][e][c] = s[c];
+    red[g][e][V] = d;
+    __syncthreads();
+    if (g) return;
 #pragma unroll
-  for (int z = 1; z < 8; ++z) {
+    for (int z = 1; z < G; ++z) {
 #pragma unroll
-    for (int c = 0; c < V; ++c) s[c] += red[z][e][c];
-    d += red[z][e][V];
+      for (int c = 0; c < V; ++c) s[c] += red[z][e][c];
+      d += red[z][e][V];
+    }
   }
+  if (i >= nk) return;
+  float o[V];
 #pragma unroll
   for (int c = 0; c < V; ++c) {
-    if (a.scale) s[c] *= a.scale[k + c];
-    if (a.shift) s[c] = fmaf(a.shift[k + c], d, s[c]);
-    float *o = a.dw + i + c;
-    *o = a.accumulate ? *o + s[c] : s[c];
+    o[c] = s[c];
+    if (a.scale) o[c] *= a.scale[k + c];
+    if (a.shift) o[c] = fmaf(a.shift[k + c], d, o[c]);
+    if (a.accumulate) o[c] += a.dw[i + c];
   }
+#pragma unroll
+  for (int c = 0; c < V; ++c) a.dw[i + c] = o[c];
   if (k == 0 && a.db) a.db[n] = a.accumulate ? a.db[n] + d : d;
 }
 
-// Tile width and rows per split.
+#ifndef WG_MIN
+#define WG_MIN 256
+#endif
+constexpr int kMinRows = WG_MIN;
+// Tile width and splits of the rows.
 struct Split {
   int tile, splits;
-  int64_t chunk;
 };
-Split split_of(int64_t rows, int64_t n, int64_t k) {
+Split split_of(int64_t rows, int64_t n, int64_t k, int32_t dtype) {
   Split r;
   auto tiles = [&](int w) { return ((n + w - 1) / w) * ((k + w - 1) / w); };
-  r.tile = n > 128 && k > 128 && tiles(256) * std::max<int64_t>(1, rows / 1024) >= 256 ? 256 : 128;
+  r.tile = dtype == LRCNN_BF16 && tiles(256) >= 16 && rows * tiles(256) >= 256 * 256 ? 256 : 128;
   int64_t s = std::max<int64_t>(1, (r.tile == 256 ? 256 : 512) / tiles(r.tile));
-  s = std::min(s, std::max<int64_t>(1, rows / 256));
-  r.chunk = ((rows + s - 1) / s + kStep - 1) / kStep * kStep;
-  if (r.chunk < kStep) r.chunk = kStep;
-  r.splits = (int)std::max<int64_t>(1, (rows + r.chunk - 1) / r.chunk);
+  // at most 2^31 steps each
+  s = std::max(s, (rows / kStep) >> 30);
+  r.splits = (int)std::min(s, std::max<int64_t>(1, rows / kMinRows));
   return r;
 }
-size_t wgrad_ws(int64_t rows, int64_t n, int64_t k) {
-  const Split s = split_of(rows, n, k);
+size_t wgrad_ws(int64_t rows, int64_t n, int64_t k, int32_t dtype) {
+  const Split s = split_of(rows, n, k, dtype);
   return s.splits == 1 ? 0 : a256((size_t)s.splits * n * k * 4) + a256((size_t)s.splits * n * 4);
 }
 
@@ -369,6 +565,8 @@ int wgrad_shape(int64_t rows, int64_t n_in, int64_t n_out, int32_t dtype) {
   int st = take_shape(rows, n_in, dtype);
   if (st == LRCNN_OK) st = take_shape(rows, n_out, dtype);
   if (st == LRCNN_OK) st = take_shape(n_out, n_in, dtype);
+  if (st == LRCNN_OK && (n_in > kMaxFeatures || n_out > kMaxFeatures))
+    st = lrcnn_fail(LRCNN_ESHAPE, "more than 2^24 features");
   return st;
 }
 
@@ -387,7 +585,7 @@ extern "C" int lrcnn_linear_wgrad_workspace_bytes(int64_t rows, int64_t n_in, in
                                                   int32_t dtype, size_t *bytes) {
   if (!bytes) return lrcnn_fail(LRCNN_EINVAL, "null output");
   TRY(wgrad_shape(rows, n_in, n_out, dtype));
-  *bytes = wgrad_ws(rows, n_out, n_in);
+  *bytes = wgrad_ws(rows, n_out, n_in, dtype);
   return LRCNN_OK;
 }
 
@@ -399,19 +597,21 @@ extern "C" int lrcnn_linear_wgrad(int64_t rows, int64_t n_in, int64_t n_out, int
   TRY(wgrad_shape(rows, n_in, n_out, dtype));
   WgArgs a{};
   TRY(take("dy", dy, lddy, n_out, dtype == LRCNN_BF16 ? 2 : 4, rows > 0, &a.dy));
+  if (rows > 0 && a.dy.ld > kMaxFeatures)
+    return lrcnn_fail(LRCNN_ESHAPE, "dy: row stride of more than 2^24");
   TRY(take_ckpt("ckpt", ckpt, rows > 0));
   TRY(take_f32("scale", scale, false));
   TRY(take_f32("shift", shift, false));
   TRY(take_f32("dw", dw, true));
   TRY(take_f32("db", db, false));
-  const Split sp = split_of(rows, n_out, n_in);
-  const size_t need = wgrad_ws(rows, n_out, n_in);
+  const Split sp = split_of(rows, n_out, n_in, dtype);
+  const size_t need = wgrad_ws(rows, n_out, n_in, dtype);
   if (need && (!workspace || ((uintptr_t)workspace & 15)))
     return lrcnn_fail(LRCNN_EINVAL, "workspace null or misaligned");
   if (ws_bytes < need)
     return lrcnn_fail(LRCNN_EWORKSPACE, "workspace needs " + std::to_string(need) +
                                             " bytes, got " + std::to_string(ws_bytes));
-  a.rows = rows, a.n = (int)n_out, a.k = (int)n_in, a.chunk = sp.chunk;
+  a.rows = rows, a.n = (int)n_out, a.k = (int)n_in, a.splits = sp.splits;
   a.q = ckpt_of(ckpt, rows, n_in);
   a.q.pitch = pitch_of(n_in);
   a.scale = scale, a.shift = shift, a.dw = dw, a.db = db, a.accumulate = accumulate != 0;
@@ -426,17 +626,39 @@ extern "C" int lrcnn_linear_wgrad(int64_t rows, int64_t n_in, int64_t n_out, int
   hipStream_t s = (hipStream_t)stream;
   auto run = [&](auto *t) {
     using T = std::remove_pointer_t<decltype(t)>;
-    if (sp.tile == 256) wgrad8_kernel<T, 256><<<grid, 256, 0, s>>>(a);
-    else wgrad8_kernel<T, 128><<<grid, 256, 0, s>>>(a);
+    auto go = [&](auto w, auto c) {
+      wgrad8_kernel<T, w.value, c.value><<<grid, 256, 0, s>>>(a);
+    };
+    std::integral_constant<int, 256> w256;
+    std::integral_constant<int, 128> w128;
+    std::integral_constant<int, COLS_WHOLE> whole;
+    std::integral_constant<int, COLS_SHIFT> shift;
+    std::integral_constant<int, COLS_EACH> each;
+    if constexpr (std::is_same<T, bf16>::value) {
+      if (sp.tile == 256) {
+        if (n_out % 8 == 0) go(w256, whole);
+        else go(w256, shift);
+        return;
+      }
+    }
+    if (n_out < 8) go(w128, each);
+    else if (n_out % 8 == 0) go(w128, whole);
+    else go(w128, shift);
   };
   if (dtype == LRCNN_BF16) run((bf16 *)nullptr);
   else run((float *)nullptr);
   if (sp.splits > 1) {
     const int64_t nk = n_out * n_in;
-    if (n_in % 4 == 0 && ((uintptr_t)workspace & 15) == 0)
-      wgrad8_join_kernel<4><<<(unsigned)((nk / 4 + 31) / 32), 256, 0, s>>>(a, sp.splits);
-    else
-      wgrad8_join_kernel<1><<<(unsigned)((nk + 31) / 32), 256, 0, s>>>(a, sp.splits);
+    auto join = [&](auto v, auto g) {
+      constexpr int E = 256 / g.value * v.value;
+      wgrad8_join_kernel<v.value, g.value><<<(unsigned)((nk + E - 1) / E), 256, 0, s>>>(a, sp.splits);
+    };
+    auto by_groups = [&](auto v) {
+      if (sp.splits <= 8) join(v, std::integral_constant<int, 1>());
+      else join(v, std::integral_constant<int, 8>());
+    };
+    if (n_in % 4 == 0) by_groups(std::integral_constant<int, 4>());
+    else by_groups(std::integral_constant<int, 1>());
   }
   return launched("linear_wgrad");
 }
