@@ -284,6 +284,12 @@ def _stream(stream):
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _raw_stream(stream, like):
+    """The stream as a number: torch's current one of the tensors' device, asked
+    for without making a Stream object (1 us of a call's 8)."""
+    return torch._C._cuda_getCurrentRawStream(like[2]) if stream is None else stream
+
+
 def lrcnn_forward_rows(plan, x, weights, scales, shifts, y, workspace, masks=None,
                        stream=None):
     """weights/scales/shifts/masks: per-node lists (None where unused)."""
@@ -357,60 +363,70 @@ def _einval(msg):
     raise LrcnnError(-1, msg)
 
 
-def _dtype_of(name, t):
-    code = _DTYPES.get(t.dtype)
+def _first(name, t):
+    """(shape, dtype, device index, library dtype, pointer, row stride) of the
+    matrix that the call's other tensors have to agree with."""
+    shape, dtype = t.shape, t.dtype
+    if len(shape) != 2:
+        _einval(f"{name} must have two dimensions")
+    if shape[1] < 1:
+        raise LrcnnError(-2, f"{name} has no columns")
+    code = _DTYPES.get(dtype)
     if code is None:
         raise LrcnnError(-6, f"{name}: dtype must be float32 or bfloat16")
-    return code
+    like = (shape, dtype, t.get_device())
+    return (*like, code, t.data_ptr(), _ld(name, t))
+
+
+def _ld(name, t):
+    """Row stride of a matrix (0: dense)."""
+    if t.is_contiguous():
+        return 0
+    rows, cols = t.shape
+    ld, one = t.stride()
+    if (one != 1 and cols > 1) or (ld < cols and rows > 1):
+        _einval(f"{name}: columns must be next to each other, rows apart")
+    return ld if rows > 1 else 0
 
 
 def _mat(name, t, like):
-    """Pointer and row stride of a matrix of like's shape, dtype and device (None:
-    absent)."""
+    """Pointer and row stride of a matrix of the first one's shape, dtype and device
+    (None: absent)."""
     if t is None:
         return None, 0
-    if t.shape != like.shape or t.dtype != like.dtype or t.device != like.device:
-        _einval(f"{name} must be a matrix like {tuple(like.shape)} {like.dtype} on {like.device}")
-    ld, one = t.stride()
-    rows, cols = t.shape
-    if (one != 1 and cols > 1) or (ld < cols and rows > 1):
-        _einval(f"{name}: columns must be next to each other, rows apart")
-    return t.data_ptr(), ld if rows > 1 else 0
-
-
-def _shape(name, t):
-    if t.dim() != 2:
-        _einval(f"{name} must have two dimensions")
-    if t.shape[1] < 1:
-        raise LrcnnError(-2, f"{name} has no columns")
-    return t.shape
+    if t.shape != like[0] or t.dtype is not like[1] or t.get_device() != like[2]:
+        _einval(f"{name} must be a matrix {tuple(like[0])} of {like[1]} on the same device")
+    return t.data_ptr(), _ld(name, t)
 
 
 def _vec(name, t, n, like):
     """Pointer of a dense float32 vector of n elements (None: absent)."""
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous() \
-            or t.device != like.device:
-        _einval(f"{name} must be {n} dense float32 values on {like.device}")
+    if t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous() \
+            or t.get_device() != like[2]:
+        _einval(f"{name} must be {n} dense float32 values on the same device")
     return t.data_ptr()
 
 
-def _bytes(name, t, need, like, code):
-    """Pointer of a byte buffer of at least `need` bytes (None: absent)."""
+def _bytes(name, t, like):
+    """Pointer and size of a byte buffer (None: absent)."""
     if t is None:
-        return None
-    if t.dtype != torch.uint8 or not t.is_contiguous() or t.device != like.device:
-        _einval(f"{name} must be dense uint8 on {like.device}")
-    if t.numel() < need:
-        raise LrcnnError(code, f"{name} needs {need} bytes, got {t.numel()}")
-    return t.data_ptr()
+        return None, 0
+    if t.dtype is not torch.uint8 or not t.is_contiguous() or t.get_device() != like[2]:
+        _einval(f"{name} must be dense uint8 on the same device")
+    return t.data_ptr(), t.numel()
 
 
 def _ckpt(name, t, shape, like):
+    """Pointer of the checkpoint of a matrix of that shape (None: absent)."""
     if t is None:
         return None
-    return _bytes(name, t, lrcnn_act8_bytes(*shape), like, -1)
+    p, n = _bytes(name, t, like)
+    codes = shape[0] * (shape[1] + 31 & -32)
+    if n < (codes + 255 & -256) + (codes // 32 + 255 & -256):
+        _einval(f"{name} is smaller than the checkpoint of {tuple(shape)}")
+    return p
 
 
 def _query(fn, *args):
@@ -426,33 +442,34 @@ def lrcnn_act8_bytes(rows, cols):
 
 def lrcnn_act8_pack(x, ckpt, stream=None):
     """ckpt (uint8, lrcnn_act8_bytes) = the 8-bit checkpoint of x."""
-    rows, cols = _shape("x", x)
-    dt, (px, ldx) = _dtype_of("x", x), _mat("x", x, x)
-    _check(LIB.lrcnn_act8_pack(rows, cols, dt, px, ldx, _ckpt("ckpt", ckpt, x.shape, x),
-                               _stream(stream)))
+    like = _first("x", x)
+    shape, _, _, dt, px, ldx = like
+    _check(LIB.lrcnn_act8_pack(shape[0], shape[1], dt, px, ldx, _ckpt("ckpt", ckpt, shape, like),
+                               _raw_stream(stream, like)))
 
 
 def lrcnn_act8_unpack(ckpt, y, stream=None):
     """y = what the checkpoint of a matrix of y's shape stands for."""
-    rows, cols = _shape("y", y)
-    dt, (py, ldy) = _dtype_of("y", y), _mat("y", y, y)
-    _check(LIB.lrcnn_act8_unpack(rows, cols, dt, _ckpt("ckpt", ckpt, y.shape, y), py, ldy,
-                                 _stream(stream)))
+    like = _first("y", y)
+    shape, _, _, dt, py, ldy = like
+    _check(LIB.lrcnn_act8_unpack(shape[0], shape[1], dt, _ckpt("ckpt", ckpt, shape, like), py, ldy,
+                                 _raw_stream(stream, like)))
 
 
 def lrcnn_layer_norm_forward(x, gamma, beta, eps, y, residual=None, total=None, mean=None,
                              rstd=None, ckpt=None, stream=None):
     """y = layer norm of the rows of x (+ residual: their sum goes to total);
     mean, rstd per row; ckpt: the checkpoint of the normalised rows."""
-    rows, cols = _shape("x", x)
-    dt, (px, ldx) = _dtype_of("x", x), _mat("x", x, x)
-    pr, ldr = _mat("residual", residual, x)
-    pt, ldt = _mat("total", total, x)
-    py, ldy = _mat("y", y, x)
+    like = _first("x", x)
+    shape, _, _, dt, px, ldx = like
+    rows, cols = shape
+    pr, ldr = _mat("residual", residual, like)
+    pt, ldt = _mat("total", total, like)
+    py, ldy = _mat("y", y, like)
     _check(LIB.lrcnn_layer_norm_forward(
-        rows, cols, dt, px, ldx, pr, ldr, _vec("gamma", gamma, cols, x),
-        _vec("beta", beta, cols, x), eps, pt, ldt, py, ldy, _vec("mean", mean, rows, x),
-        _vec("rstd", rstd, rows, x), _ckpt("ckpt", ckpt, x.shape, x), _stream(stream)))
+        rows, cols, dt, px, ldx, pr, ldr, _vec("gamma", gamma, cols, like),
+        _vec("beta", beta, cols, like), eps, pt, ldt, py, ldy, _vec("mean", mean, rows, like),
+        _vec("rstd", rstd, rows, like), _ckpt("ckpt", ckpt, shape, like), _raw_stream(stream, like)))
 
 
 def lrcnn_layer_norm_workspace_bytes(rows, cols):
@@ -463,47 +480,47 @@ def lrcnn_layer_norm_backward(dy, rstd, gamma, dx, dgamma=None, dbeta=None, work
                               x=None, mean=None, ckpt=None, dres=None, accumulate=False,
                               stream=None):
     """dx (+ dres), dgamma and dbeta from dy and either (x, mean) or ckpt."""
-    rows, cols = _shape("dy", dy)
-    dt, (pdy, lddy) = _dtype_of("dy", dy), _mat("dy", dy, dy)
-    px, ldx = _mat("x", x, dy)
-    pr, ldr = _mat("dres", dres, dy)
-    pdx, lddx = _mat("dx", dx, dy)
+    like = _first("dy", dy)
+    shape, _, _, dt, pdy, lddy = like
+    rows, cols = shape
+    px, ldx = _mat("x", x, like)
+    pr, ldr = _mat("dres", dres, like)
+    pdx, lddx = _mat("dx", dx, like)
+    pw, nw = _bytes("workspace", workspace, like)
     _check(LIB.lrcnn_layer_norm_backward(
-        rows, cols, dt, pdy, lddy, px, ldx, _vec("mean", mean, rows, dy),
-        _ckpt("ckpt", ckpt, dy.shape, dy), _vec("rstd", rstd, rows, dy),
-        _vec("gamma", gamma, cols, dy), pr, ldr, pdx, lddx, _vec("dgamma", dgamma, cols, dy),
-        _vec("dbeta", dbeta, cols, dy), 1 if accumulate else 0,
-        _bytes("workspace", workspace, 0, dy, -4),
-        0 if workspace is None else workspace.numel(), _stream(stream)))
+        rows, cols, dt, pdy, lddy, px, ldx, _vec("mean", mean, rows, like),
+        _ckpt("ckpt", ckpt, shape, like), _vec("rstd", rstd, rows, like),
+        _vec("gamma", gamma, cols, like), pr, ldr, pdx, lddx, _vec("dgamma", dgamma, cols, like),
+        _vec("dbeta", dbeta, cols, like), 1 if accumulate else 0, pw, nw, _raw_stream(stream, like)))
 
 
 def lrcnn_activation_forward(kind, u, a=None, v=None, ckpt_u=None, ckpt_v=None, ckpt_a=None,
                              stream=None):
     """a = f(u) (times v), and the checkpoints of u, v and a that are given."""
-    rows, cols = _shape("u", u)
-    dt, (pu, ldu) = _dtype_of("u", u), _mat("u", u, u)
-    pv, ldv = _mat("v", v, u)
-    pa, lda = _mat("a", a, u)
+    like = _first("u", u)
+    shape, _, _, dt, pu, ldu = like
+    pv, ldv = _mat("v", v, like)
+    pa, lda = _mat("a", a, like)
     _check(LIB.lrcnn_activation_forward(
-        rows, cols, dt, kind, pu, ldu, pv, ldv, pa, lda, _ckpt("ckpt_u", ckpt_u, u.shape, u),
-        _ckpt("ckpt_v", ckpt_v, u.shape, u), _ckpt("ckpt_a", ckpt_a, u.shape, u),
-        _stream(stream)))
+        shape[0], shape[1], dt, kind, pu, ldu, pv, ldv, pa, lda,
+        _ckpt("ckpt_u", ckpt_u, shape, like), _ckpt("ckpt_v", ckpt_v, shape, like),
+        _ckpt("ckpt_a", ckpt_a, shape, like), _raw_stream(stream, like)))
 
 
 def lrcnn_activation_backward(kind, da, du, u=None, v=None, ckpt_u=None, ckpt_v=None, dv=None,
                               ckpt_a=None, stream=None):
     """du (and dv) from da and either u (and v) or their checkpoints; ckpt_a:
     receives the checkpoint of the activation's output."""
-    rows, cols = _shape("da", da)
-    dt, (pda, ldda) = _dtype_of("da", da), _mat("da", da, da)
-    pu, ldu = _mat("u", u, da)
-    pv, ldv = _mat("v", v, da)
-    pdu, lddu = _mat("du", du, da)
-    pdv, lddv = _mat("dv", dv, da)
+    like = _first("da", da)
+    shape, _, _, dt, pda, ldda = like
+    pu, ldu = _mat("u", u, like)
+    pv, ldv = _mat("v", v, like)
+    pdu, lddu = _mat("du", du, like)
+    pdv, lddv = _mat("dv", dv, like)
     _check(LIB.lrcnn_activation_backward(
-        rows, cols, dt, kind, pda, ldda, pu, ldu, pv, ldv,
-        _ckpt("ckpt_u", ckpt_u, da.shape, da), _ckpt("ckpt_v", ckpt_v, da.shape, da), pdu, lddu,
-        pdv, lddv, _ckpt("ckpt_a", ckpt_a, da.shape, da), _stream(stream)))
+        shape[0], shape[1], dt, kind, pda, ldda, pu, ldu, pv, ldv,
+        _ckpt("ckpt_u", ckpt_u, shape, like), _ckpt("ckpt_v", ckpt_v, shape, like), pdu, lddu,
+        pdv, lddv, _ckpt("ckpt_a", ckpt_a, shape, like), _raw_stream(stream, like)))
 
 
 def lrcnn_linear_wgrad_workspace_bytes(rows, n_in, n_out, dtype=F32):
@@ -515,17 +532,17 @@ def lrcnn_linear_wgrad(dy, ckpt, dw, workspace=None, db=None, scale=None, shift=
     """dw [n_out][n_in] and db [n_out] of a linear layer from dy [rows][n_out] and
     the checkpoint [rows][n_in] of its input (the input being scale times that
     plus shift, per column)."""
-    rows, n_out = _shape("dy", dy)
-    dt, (pdy, lddy) = _dtype_of("dy", dy), _mat("dy", dy, dy)
+    like = _first("dy", dy)
+    (rows, n_out), _, _, dt, pdy, lddy = like
     if dw.dim() != 2 or dw.shape[0] != n_out:
         _einval("dw must be [n_out][n_in]")
-    n_in = _shape("dw", dw)[1]
+    n_in = dw.shape[1]
+    pw, nw = _bytes("workspace", workspace, like)
     _check(LIB.lrcnn_linear_wgrad(
-        rows, n_in, n_out, dt, pdy, lddy, _ckpt("ckpt", ckpt, (rows, n_in), dy),
-        _vec("scale", scale, n_in, dy), _vec("shift", shift, n_in, dy),
-        _vec("dw", dw, n_out * n_in, dy), _vec("db", db, n_out, dy), 1 if accumulate else 0,
-        _bytes("workspace", workspace, 0, dy, -4),
-        0 if workspace is None else workspace.numel(), _stream(stream)))
+        rows, n_in, n_out, dt, pdy, lddy, _ckpt("ckpt", ckpt, (rows, n_in), like),
+        _vec("scale", scale, n_in, like), _vec("shift", shift, n_in, like),
+        _vec("dw", dw, n_out * n_in, like), _vec("db", db, n_out, like), 1 if accumulate else 0,
+        pw, nw, _raw_stream(stream, like)))
 
 
 def lrcnn_debug_dry_run(on):
