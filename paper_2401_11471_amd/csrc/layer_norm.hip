@@ -19,8 +19,16 @@ namespace act8 {
 namespace {
 
 constexpr int kMaxNormCols = 16384;
-// backward: blocks that each keep a running dgamma and dbeta of their rows
-constexpr int kMaxParts = 512;
+// Backward: blocks that each keep a running dgamma and dbeta of their rows, three
+// to a CU, as many as fit with four rows in flight: 67800 x 2048 bf16 from a
+// checkpoint with dres 192 us (512 blocks 224, 1024 231, 2048 209; two rows in
+// flight and 1024 blocks 190, but float32 30000 x 2048 171 us to 152).
+constexpr int kMaxParts = 768;
+// Forward: blocks that walk the rows. Rows of one vector a thread take many
+// (67800 x 2048 bf16 with residual and checkpoint: 2048 blocks 267 us, 8192
+// 234, 16384 230, 65536 235; 512 columns 61.8, 55.5, 55.5, 55.2), wider ones few
+// (20000 x 4096 bf16: 2048 blocks 78 us, 16384 93).
+constexpr int kFwdBlocks = 8192, kFwdBlocksWide = 2048;
 
 // Sum over a wave, the same in every lane: adds inside rows of 16 lanes, then
 // across rows, a fixed tree.
@@ -414,7 +422,7 @@ extern "C" int lrcnn_layer_norm_forward(int64_t rows, int64_t cols, int32_t dtyp
     constexpr int TPR = tpr.value, NV = nv.value, BS = TPR > 256 ? TPR : 256;
     constexpr int R = NV == 1 ? 2 : 1;
     const int64_t per = (int64_t)(BS / TPR) * R;
-    const unsigned g = (unsigned)std::min<int64_t>((rows + per - 1) / per, 2048 * 256 / BS);
+    const unsigned g = (unsigned)std::min<int64_t>((rows + per - 1) / per, (NV == 1 ? kFwdBlocks : kFwdBlocksWide) * 256 / BS);
     if (dtype == LRCNN_BF16)
       ln_fwd_kernel<bf16, TPR, NV, R><<<g, BS, 0, (hipStream_t)stream>>>(a);
     else
