@@ -23,12 +23,14 @@ namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int64_t kMaxFeatures = 1 << 24;  // 31 rows within 32-bit offsets
+constexpr int64_t kMaxWgradRows = 1 << 30;
 constexpr int kStep = 32;  // rows of dy and of the checkpoint per step
 
 struct WgArgs {
-  int64_t rows;
-  int n, k;             // outputs, inputs
+  int rows, n, k;       // n outputs, k inputs
   int splits;           // split z takes the steps z, z + splits, ...
+  int gx, gy;           // tiles of n and of k
+  FastDiv tiles, panel, rest, stride;  // by gx gy, 8 gy, gx mod 8, 32 splits
   Mat dy;
   Ckpt q;
   const float *scale, *shift;
@@ -84,16 +86,20 @@ __device__ __forceinline__ void each(F &&f) {
   }
 }
 
-// Tiles run through a panel of eight tiles of n before the next k, so that
-// the run of tiles an XCD works on shares rows of both operands in its L2.
-__device__ __forceinline__ TileId panel_tile() {
-  const int gx = gridDim.x, gy = gridDim.y;
-  TileId t = xcd_tile(false);
-  const int id = t.x + gx * t.y, panel = id / (8 * gy), r = id - panel * 8 * gy;
-  const int w = min(8, gx - 8 * panel);
-  t.y = r / w;
-  t.x = 8 * panel + (r - t.y * w);
-  return t;
+// The tile of this workgroup. Workgroups go to the eight XCDs in turn; each XCD
+// gets one run of tiles in order: splits last, and within one split through a
+// panel of eight tiles of n before the next k, so that the tiles an XCD works
+// on share rows of both operands in its L2.
+__device__ __forceinline__ TileId panel_tile(const WgArgs &a) {
+  const uint32_t total = gridDim.x, w = blockIdx.x;
+  const uint32_t q = total >> 3, o = total & 7, c = w & 7, k = w >> 3;
+  const uint32_t id = c < o ? c * (q + 1) + k : o * (q + 1) + (c - o) * q + k;
+  uint32_t z, t, p, r, x, y;
+  fdiv_qr(id, a.tiles, z, t);
+  fdiv_qr(t, a.panel, p, r);
+  if (8 * p + 8 <= (uint32_t)a.gx) y = r >> 3, x = r & 7;
+  else fdiv_qr(r, a.rest, y, x);
+  return TileId{(int)(8 * p + x), (int)y, (int)z};
 }
 
 constexpr int least(int a, int b) { return a < b ? a : b; }
@@ -121,7 +127,7 @@ enum Cols {
 template <typename T, int W, int COLS>
 __global__ __launch_bounds__(256, W == 256 ? 1 : 2) void wgrad8_kernel(WgArgs a) {
   constexpr int P = std::is_same<T, float>::value ? 3 : 1;  // pieces of dy
-  constexpr int ST = P == 1 ? 3 : 2;                         // LDS tiles and load slots
+  constexpr int ST = W == 256 ? 3 : 2;                       // LDS tiles and load slots
   constexpr int NB = W / 64;                                 // 32 x 32 blocks per wave and side
   constexpr int U = 2 * P;                                   // units per step
   constexpr int LA = W / 8, RA = 256 / LA, NA = kStep / RA;  // dy: lanes, rows, passes
@@ -134,13 +140,13 @@ __global__ __launch_bounds__(256, W == 256 ? 1 : 2) void wgrad8_kernel(WgArgs a)
   __shared__ float dbs[W];
   const int tid = threadIdx.x, lane = tid & 63,
             wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const TileId tl = panel_tile();
+  const TileId tl = panel_tile(a);
   const int n0 = tl.x * W, k0 = tl.y * W;
   // This split's steps: every splits-th run of kStep rows, so that the
   // workgroups together read one window of rows that moves on
-  const int64_t stride = (int64_t)a.splits * kStep, first = (int64_t)tl.z * kStep;
-  const int steps = first < a.rows ? (int)((a.rows - first + stride - 1) / stride) : 0;
-  const int some = (int)min(a.rows, (int64_t)kStep);  // rows a step can read
+  const int stride = a.splits * kStep, first = tl.z * kStep;
+  const int steps = first < a.rows ? (int)fdiv_q(a.rows - 1 - first, a.stride) + 1 : 0;
+  const int some = min(a.rows, kStep);  // rows a step can read
   const int ar = tid / LA, ac = n0 + (tid % LA) * 8;
   const int br = tid / LB, bc = k0 + (tid % LB) * 16;
   int al = ac < a.n ? ac : 0, down = 0;
@@ -175,10 +181,10 @@ __global__ __launch_bounds__(256, W == 256 ? 1 : 2) void wgrad8_kernel(WgArgs a)
     ge = (const char *)a.q.e + m * pe_ld;
   };
   // this split's last step is not whole: it comes first, `zero` rows early
-  const int64_t over = first + steps * stride - stride + kStep - a.rows;
+  const int over = first + (steps - 1) * stride + kStep - a.rows;
   const bool odd = over > 0;
-  const int zero = odd && a.rows >= kStep ? (int)over : 0;
-  place(odd ? max(a.rows - kStep, (int64_t)0) : first);
+  const int zero = odd && a.rows >= kStep ? over : 0;
+  place(odd ? max(a.rows - kStep, 0) : first);
   // (past the end the last step again. Scalar bases that the compiler may not
   // fold into one address per lane and load.)
   auto advance = [&]() {
@@ -436,13 +442,14 @@ __global__ __launch_bounds__(256, W == 256 ? 1 : 2) void wgrad8_kernel(WgArgs a)
   constexpr int V = W / 128;
   float *own = (float *)smem + wave * 32 * EP;
   float *out = a.part ? a.part + (int64_t)tl.z * a.n * a.k : a.dw;
-  const int kk = k0 + wk + V * lane;
+  typedef __attribute__((address_space(1))) float g_float;
+  const bool acc_in = a.accumulate && !a.part;
   float sc[V], sh[V];
 #pragma unroll
   for (int c = 0; c < V; ++c) {
-    const bool in = kk + c < a.k && !a.part;
-    sc[c] = in && a.scale ? a.scale[kk + c] : 1.f;
-    sh[c] = in && a.shift ? a.shift[kk + c] : 0.f;
+    const int kk = k0 + wk + 64 * c + lane;
+    sc[c] = kk < a.k && !a.part && a.scale ? a.scale[kk] : 1.f;
+    sh[c] = kk < a.k && !a.part && a.shift ? a.shift[kk] : 0.f;
   }
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
@@ -453,34 +460,32 @@ __global__ __launch_bounds__(256, W == 256 ? 1 : 2) void wgrad8_kernel(WgArgs a)
       for (int v = 0; v < 16; ++v) own[acc_row(v, lane) * EP + 32 * j + (lane & 31)] = acc[i][j][v];
     __builtin_amdgcn_wave_barrier();
     const int nb = wn + 32 * i, rows = min(32, a.n - n0 - nb);
-    typedef __attribute__((address_space(1))) float g_float;
-    g_float *at = (g_float *)out + (int64_t)(n0 + nb) * a.k + kk;
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+      const int kk = k0 + wk + 64 * c + lane;
+      if (kk >= a.k) continue;
+      const float *from = own + 64 * c + lane, *db = dbs + nb;
+      g_float *to = (g_float *)out + (int64_t)(n0 + nb) * a.k + kk;
+      int r = 0;
 #pragma unroll 1
-    for (int r = 0; r < rows; r += 8) {
-      // eight rows on their way at a time
-      float x[8][V], b[8], old[8][V];
+      for (; r + 8 <= rows; r += 8) {  // eight rows on their way at a time
+        float x[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        b[e] = dbs[nb + r + e];
+        for (int e = 0; e < 8; ++e) x[e] = fmaf(sh[c], db[r + e], from[(r + e) * EP] * sc[c]);
+        if (acc_in) {
 #pragma unroll
-        for (int c = 0; c < V; ++c) {
-          x[e][c] = own[(r + e) * EP + V * lane + c];
-          old[e][c] = 0.f;
+          for (int e = 0; e < 8; ++e) x[e] += to[e * (int64_t)a.k];
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) to[e * (int64_t)a.k] = x[e];
+        to += 8 * (int64_t)a.k;
       }
-      if (a.accumulate && !a.part) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-#pragma unroll
-          for (int c = 0; c < V; ++c)
-            if (r + e < rows && kk + c < a.k) old[e][c] = at[(int64_t)(r + e) * a.k + c];
+#pragma unroll 1
+      for (; r < rows; ++r) {
+        const float x = fmaf(sh[c], db[r], from[r * EP] * sc[c]);
+        *to = acc_in ? *to + x : x;
+        to += a.k;
       }
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-#pragma unroll
-        for (int c = 0; c < V; ++c)
-          if (r + e < rows && kk + c < a.k)
-            at[(int64_t)(r + e) * a.k + c] = fmaf(sh[c], b[e], x[e][c] * sc[c]) + old[e][c];
     }
   }
 }
@@ -538,26 +543,41 @@ __global__ __launch_bounds__(256) void wgrad8_join_kernel(WgArgs a, int splits) 
   if (k == 0 && a.db) a.db[n] = a.accumulate ? a.db[n] + d : d;
 }
 
-#ifndef WG_MIN
-#define WG_MIN 256
-#endif
-constexpr int kMinRows = WG_MIN;
-// Tile width and splits of the rows.
+// Tile width and splits of the rows: the least estimated time, in us, of
+//   steps of a workgroup x time of a step x workgroups of a CU, and, if split,
+//   the join's launch and the partial sums written and read.
+// A step of 32 rows takes 0.98 (256-wide bf16 tile, one workgroup a CU), 0.35
+// (128-wide) or 0.82 (128-wide float32); two workgroups a CU share it at 0.85 of
+// twice the time. Measured for splits of the 128-wide tile (us): 1568 x 256 x
+// 256 bf16 by 3 15.2, 6 12.7, 12 11.3, 24 12.3; 392 x 512 x 2048 bf16 by 1 11.8,
+// 3 17.3, 6 23.4; 784 x 64 x 64 float32 by 1 28.1, 3 17.1, 12 12.2; for the tiles:
+// 67800 x 2048 x 8192 bf16 2784 and 2083, 67800 x 512 x 2048 195 and 188,
+// 540000 x 256 x 256 121 and 130; float32 67800 x 512 x 512 137 and 151 (a
+// 256-wide float32 tile spills registers and is not kept).
 struct Split {
   int tile, splits;
 };
 Split split_of(int64_t rows, int64_t n, int64_t k, int32_t dtype) {
-  Split r;
-  auto tiles = [&](int w) { return ((n + w - 1) / w) * ((k + w - 1) / w); };
-  r.tile = dtype == LRCNN_BF16 && tiles(256) >= 16 && rows * tiles(256) >= 256 * 256 ? 256 : 128;
-  int64_t s = std::max<int64_t>(1, (r.tile == 256 ? 256 : 512) / tiles(r.tile));
-  // at most 2^31 steps each
-  s = std::max(s, (rows / kStep) >> 30);
-  r.splits = (int)std::min(s, std::max<int64_t>(1, rows / kMinRows));
-  return r;
+  const int64_t steps = (rows + kStep - 1) / kStep;
+  Split best{128, 1};
+  double least_us = -1;
+  for (int tile = 128; tile <= (dtype == LRCNN_BF16 ? 256 : 128); tile *= 2) {
+    const int64_t tiles = ((n + tile - 1) / tile) * ((k + tile - 1) / tile);
+    const double step_us = tile == 256 ? 0.98 : dtype == LRCNN_BF16 ? 0.35 : 0.82;
+    auto consider = [&](int64_t s) {
+      if (s < 1 || (s > 1 && (s > steps || s * tiles > 1024))) return;
+      const double per_cu = (double)((tiles * s + 255) / 256);
+      const double share = tile == 128 && per_cu > 1 ? 0.85 : 1.0;
+      double us = (double)((steps + s - 1) / s) * step_us * per_cu * share;
+      if (s > 1) us += 2.5 + 2.2e-6 * (double)s * (double)n * (double)k;
+      if (least_us < 0 || us < least_us) least_us = us, best = Split{tile, (int)s};
+    };
+    for (int64_t s = 1; s <= 512; s += s < 8 ? 1 : s / 4) consider(s);
+    consider(256 / tiles), consider(512 / tiles);  // one or two workgroups on every CU
+  }
+  return best;
 }
-size_t wgrad_ws(int64_t rows, int64_t n, int64_t k, int32_t dtype) {
-  const Split s = split_of(rows, n, k, dtype);
+size_t wgrad_ws(const Split &s, int64_t n, int64_t k) {
   return s.splits == 1 ? 0 : a256((size_t)s.splits * n * k * 4) + a256((size_t)s.splits * n * 4);
 }
 
@@ -567,6 +587,8 @@ int wgrad_shape(int64_t rows, int64_t n_in, int64_t n_out, int32_t dtype) {
   if (st == LRCNN_OK) st = take_shape(n_out, n_in, dtype);
   if (st == LRCNN_OK && (n_in > kMaxFeatures || n_out > kMaxFeatures))
     st = lrcnn_fail(LRCNN_ESHAPE, "more than 2^24 features");
+  if (st == LRCNN_OK && rows > kMaxWgradRows)
+    st = lrcnn_fail(LRCNN_ESHAPE, "weight gradient over more than 2^30 rows");
   return st;
 }
 
@@ -585,7 +607,7 @@ extern "C" int lrcnn_linear_wgrad_workspace_bytes(int64_t rows, int64_t n_in, in
                                                   int32_t dtype, size_t *bytes) {
   if (!bytes) return lrcnn_fail(LRCNN_EINVAL, "null output");
   TRY(wgrad_shape(rows, n_in, n_out, dtype));
-  *bytes = wgrad_ws(rows, n_out, n_in, dtype);
+  *bytes = wgrad_ws(split_of(rows, n_out, n_in, dtype), n_out, n_in);
   return LRCNN_OK;
 }
 
@@ -605,13 +627,13 @@ extern "C" int lrcnn_linear_wgrad(int64_t rows, int64_t n_in, int64_t n_out, int
   TRY(take_f32("dw", dw, true));
   TRY(take_f32("db", db, false));
   const Split sp = split_of(rows, n_out, n_in, dtype);
-  const size_t need = wgrad_ws(rows, n_out, n_in, dtype);
+  const size_t need = wgrad_ws(sp, n_out, n_in);
   if (need && (!workspace || ((uintptr_t)workspace & 15)))
     return lrcnn_fail(LRCNN_EINVAL, "workspace null or misaligned");
   if (ws_bytes < need)
     return lrcnn_fail(LRCNN_EWORKSPACE, "workspace needs " + std::to_string(need) +
                                             " bytes, got " + std::to_string(ws_bytes));
-  a.rows = rows, a.n = (int)n_out, a.k = (int)n_in, a.splits = sp.splits;
+  a.rows = (int)rows, a.n = (int)n_out, a.k = (int)n_in, a.splits = sp.splits;
   a.q = ckpt_of(ckpt, rows, n_in);
   a.q.pitch = pitch_of(n_in);
   a.scale = scale, a.shift = shift, a.dw = dw, a.db = db, a.accumulate = accumulate != 0;
@@ -619,10 +641,14 @@ extern "C" int lrcnn_linear_wgrad(int64_t rows, int64_t n_in, int64_t n_out, int
     a.part = (float *)workspace;
     a.dbpart = (float *)((char *)workspace + a256((size_t)sp.splits * n_out * n_in * 4));
   }
-  const dim3 grid((unsigned)((n_out + sp.tile - 1) / sp.tile),
-                  (unsigned)((n_in + sp.tile - 1) / sp.tile), (unsigned)sp.splits);
-  if (grid.y > 65535 || (int64_t)grid.x * grid.y * grid.z > INT32_MAX)
-    return lrcnn_fail(LRCNN_ESHAPE, "too many features");
+  const int64_t gx = (n_out + sp.tile - 1) / sp.tile, gy = (n_in + sp.tile - 1) / sp.tile;
+  if (gx * gy * sp.splits >= (1 << 24)) return lrcnn_fail(LRCNN_ESHAPE, "too many features");
+  a.gx = (int)gx, a.gy = (int)gy;
+  a.tiles = lrcnn::fast_div((uint32_t)(gx * gy));
+  a.panel = lrcnn::fast_div((uint32_t)(8 * gy));
+  a.rest = lrcnn::fast_div((uint32_t)(gx % 8 ? gx % 8 : 8));
+  a.stride = lrcnn::fast_div((uint32_t)(lrcnn::act8::kStep * sp.splits));
+  const dim3 grid((unsigned)(gx * gy * sp.splits));
   hipStream_t s = (hipStream_t)stream;
   auto run = [&](auto *t) {
     using T = std::remove_pointer_t<decltype(t)>;
