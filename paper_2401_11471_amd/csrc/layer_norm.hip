@@ -49,15 +49,31 @@ __device__ __forceinline__ float wave_sum(float x) {
   const float d = __uint_as_float(__builtin_amdgcn_readlane(u, 63));
   return (a + b) + (c + d);
 }
+// Sum over TPR <= 32 neighbouring lanes, the same in each: swaps inside four
+// lanes, of the fours of eight, of the eights of sixteen, of the sixteens.
+template <int CTRL>
+__device__ __forceinline__ float swap_add(float x) {
+  return x + __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), CTRL, 0xf,
+                                                                0xf, true));
+}
+template <int TPR>
+__device__ __forceinline__ float lanes_sum(float x) {
+  x = swap_add<0xb1>(x);                           // lane ^ 1
+  x = swap_add<0x4e>(x);                           // lane ^ 2
+  if constexpr (TPR >= 8) x = swap_add<0x141>(x);  // 7 - lane of eight
+  if constexpr (TPR >= 16) x = swap_add<0x140>(x); // 15 - lane of sixteen
+  if constexpr (TPR >= 32) x += __shfl_xor(x, 16);
+  return x;
+}
 // N sums over the TPR threads of a row, by all threads of the block. `red`
 // has two halves, used in turn, so one barrier a call is enough.
 template <int TPR, int N>
 __device__ __forceinline__ void row_sums(float (&s)[N], float *red, int &turn) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) s[i] = wave_sum(s[i]);
+  for (int i = 0; i < N; ++i) s[i] = TPR < 64 ? lanes_sum<TPR>(s[i]) : wave_sum(s[i]);
   if constexpr (TPR > 64) {
-    constexpr int W = TPR / 64;
-    float *b = red + turn * W * N;
+    constexpr int W = TPR / 64, ALL = (TPR > 256 ? TPR : 256) / 64;  // waves of a row, a block
+    float *b = red + turn * ALL * N;
     turn ^= 1;
     const int wave = threadIdx.x >> 6;
     if ((threadIdx.x & 63) == 0) {
@@ -65,6 +81,7 @@ __device__ __forceinline__ void row_sums(float (&s)[N], float *red, int &turn) {
       for (int i = 0; i < N; ++i) b[wave * N + i] = s[i];
     }
     __syncthreads();
+    b += wave / W * W * N;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float t = b[i];
@@ -89,7 +106,7 @@ struct FwdArgs {
 template <typename T, int TPR, int NV, int R>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void ln_fwd_kernel(FwdArgs a) {
   constexpr int BS = TPR > 256 ? TPR : 256, RB = BS / TPR;
-  __shared__ float red[2 * (TPR / 64) * R];
+  __shared__ float red[2 * (BS / 64) * R];
   int turn = 0;
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   float ga[NV][8], be[NV][8];
@@ -203,7 +220,7 @@ struct BwdArgs {
 template <typename T, bool CK, int TPR, int NV, int R>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void ln_bwd_kernel(BwdArgs a) {
   constexpr int BS = TPR > 256 ? TPR : 256, RB = BS / TPR;
-  __shared__ float red[2 * (TPR / 64) * 2 * R];
+  __shared__ float red[2 * (BS / 64) * 2 * R];
   int turn = 0;
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   float ga[NV][8], dg[NV][8], db[NV][8];
@@ -356,14 +373,21 @@ __global__ __launch_bounds__(256) void ln_join_kernel(const float *part, int par
   }
 }
 
-// Threads and vectors of a row: one wave up to 512 columns, four up to 8192,
-// eight beyond.
+// Threads and vectors of a row: four to sixty-four lanes up to 512 columns, so
+// that narrow rows share a wave, two waves up to 1024, four up to 8192, eight
+// beyond. (1000000 rows bf16 forward, one wave a row and as here, us: 17 columns
+// 238 and 25, 64 columns 228 and 46; 500000 x 200 164 and 87.)
 template <typename F>
 void by_width(int cols, F &&f) {
   using std::integral_constant;
   auto go = [&](auto tpr, auto nv) { f(tpr, nv); };
 #define W(t, v) go(integral_constant<int, t>(), integral_constant<int, v>())
-  if (cols <= 512) W(64, 1);
+  if (cols <= 32) W(4, 1);
+  else if (cols <= 64) W(8, 1);
+  else if (cols <= 128) W(16, 1);
+  else if (cols <= 256) W(32, 1);
+  else if (cols <= 512) W(64, 1);
+  else if (cols <= 1024) W(128, 1);
   else if (cols <= 2048) W(256, 1);
   else if (cols <= 4096) W(256, 2);
   else if (cols <= 8192) W(256, 4);
