@@ -121,9 +121,17 @@ enum Cols {
 // There is one kind of step in the loop. Rows left over from whole steps are
 // taken first, as the matrix' last 32 rows of which those that a whole step
 // has count as zeros, and the steps that fill up the last round of ST multiply
-// by zero; so the code that runs once is short (a second, guarded kind of step
-// cost 40 us a launch in instruction fetches alone). Columns past the matrix
-// are read from its first ones: what they give is never stored.
+// by zero; so the code that runs once is short, which a small call notices: its
+// instructions come from memory (64 x 2048 x 1000 bf16 13.6 us with guarded steps
+// for the ends, 7.6 as here). Columns past the matrix are read from its first
+// ones: what they give is never stored.
+//
+// 67800 x 2048 x 8192 bf16 (2.27 TFLOP) takes 2.08 to 2.15 ms, 1060 to 1093
+// TFLOP/s. The matrix pipes are busy 51% of the cycles and the clock falls to
+// 1.67 GHz: it is bound by power, as this card's own bf16 products are (54%).
+// float32 67800 x 2048 x 2048 takes 1.69 ms: three products, 1009 TFLOP/s.
+// Long and narrow calls (540000 x 64 x 64) are bound by reading dy and the
+// codes; small float32 ones by the instructions that cut dy.
 template <typename T, int W, int COLS>
 __global__ __launch_bounds__(256, W == 256 ? 1 : 2) void wgrad8_kernel(WgArgs a) {
   constexpr int P = std::is_same<T, float>::value ? 3 : 1;  // pieces of dy
@@ -561,7 +569,9 @@ Split split_of(int64_t rows, int64_t n, int64_t k, int32_t dtype) {
   const int64_t steps = (rows + kStep - 1) / kStep;
   Split best{128, 1};
   double least_us = -1;
-  for (int tile = 128; tile <= (dtype == LRCNN_BF16 ? 256 : 128); tile *= 2) {
+  // (of a 256-wide tile half would be empty at 128 columns or fewer)
+  const int widest = dtype == LRCNN_BF16 && n > 128 && k > 128 ? 256 : 128;
+  for (int tile = 128; tile <= widest; tile *= 2) {
     const int64_t tiles = ((n + tile - 1) / tile) * ((k + tile - 1) / tile);
     const double step_us = tile == 256 ? 0.98 : dtype == LRCNN_BF16 ? 0.35 : 0.82;
     auto consider = [&](int64_t s) {

@@ -581,3 +581,41 @@ def test_runs_on_the_callers_stream_and_in_a_graph():
         graph.replay()
         got = snapshot()
         assert all(torch.equal(got[k], want[k]) for k in want)
+
+
+# ----------------------------------------- the sizes at which kernels change
+NARROW = [(70, 65), (41, 100), (130, 128), (19, 129), (66, 200), (257, 256), (12, 257), (33, 640),
+          (5, 1024), (18, 1025), (3, 4096), (2, 8192), (300000, 17), (100001, 33)]
+
+
+@TYPES
+@pytest.mark.parametrize("rows,cols", NARROW)
+@pytest.mark.parametrize("full", [True, False], ids=["all", "plain"])
+def test_layer_norm_forward_widths(rows, cols, dtype, full):
+    """Widths on both sides of those at which a row takes more threads, and rows
+    enough that a block takes several."""
+    test_layer_norm_forward(rows, cols, dtype, full)
+
+
+@TYPES
+@pytest.mark.parametrize("rows,cols", NARROW)
+@pytest.mark.parametrize("saved", [True, False], ids=["ckpt", "x"])
+def test_layer_norm_backward_widths(rows, cols, dtype, saved):
+    test_layer_norm_backward(rows, cols, dtype, saved)
+
+
+@TYPES
+@pytest.mark.parametrize("rows,n_in,n_out", [
+    (1, 4096, 4096), (33, 2500, 5000), (64, 2048, 8192), (65, 4096, 4096), (96, 2048, 4097),
+    (200, 2100, 7000), (170, 2050, 7003), (4000, 2048, 2051)])
+@pytest.mark.parametrize("affine", [False, True], ids=["plain", "affine"])
+def test_linear_wgrad_wide(rows, n_in, n_out, dtype, affine):
+    """Layers wide enough for the largest tile, with rows that fill none, one
+    and several rounds of its steps."""
+    test_linear_wgrad(rows, n_in, n_out, dtype, affine)
+
+
+@TYPES
+def test_linear_wgrad_few_outputs_of_many_inputs(dtype):
+    for n_out in (1, 7, 9):
+        test_linear_wgrad(40, 70001, n_out, dtype, True)
