@@ -5,7 +5,12 @@
 // All four are bound by HBM: two to five streams of 1 to 4 bytes an element,
 // a dozen operations each. A thread takes eight columns (16 bytes of
 // bfloat16), so a quad of lanes holds a group and its maximum takes two
-// quad moves.
+// quad moves. 1080000 x 512 bf16: pack 315 us, 5.3 TB/s, unpack 312 us; gelu
+// with a checkpoint, 67800 x 8192 bf16, 598 us, 4.7 TB/s; the backward pass of a
+// gated silu from checkpoints, 3136 x 2731 bf16, 18 us, 4.3 TB/s, partly from the
+// Infinity Cache (a device copy of 4 GiB runs at 4.84 TB/s). Eight columns a
+// thread and a thread's rows one after the other: the loads of many waves, not
+// of one, cover the latency. A call of one row takes 3.2 us, a launch's time.
 #include "act8.hpp"
 
 #include <type_traits>

@@ -7,8 +7,11 @@
 //
 // Both read a row once: it stays in registers (TPR threads of NV vectors of
 // eight columns) between its statistics and its result. Both are bound by
-// HBM. Statistics and sums are float32: the mean first, then the centred sum of
-// squares, so a large mean costs no digits of the variance.
+// HBM: 67800 x 2048 bf16 with residual and checkpoint 231 us forward (5.4 TB/s),
+// 189 and 5.5 for the join backward from the checkpoint (5.3 TB/s); one row takes
+// 3.4 us, a launch's time. Statistics and sums are float32: the mean first,
+// then the centred sum of squares, so a large mean costs no digits of the
+// variance.
 #include "act8.hpp"
 
 #include <algorithm>
@@ -24,6 +27,11 @@ constexpr int kMaxNormCols = 16384;
 // checkpoint with dres 192 us (512 blocks 224, 1024 231, 2048 209; two rows in
 // flight and 1024 blocks 190, but float32 30000 x 2048 171 us to 152).
 constexpr int kMaxParts = 768;
+// Backward, rows of one wave or less: where four rows at a time would be fewer
+// blocks than CUs, two (both launches, by four and by two, us: 1183 x 509 float32
+// 10.1 and 8.3, 12000 x 33 bf16 11.7 and 10.1, 392 x 512 float32 7.6 and 7.3; by
+// one 8.9, 14.6, 7.7; wider rows gain nothing, 1000 x 1024 bf16 10.3 and 10.5).
+constexpr int kFewParts = 256;
 // Forward: blocks that walk the rows. Rows of one vector a thread take many
 // (67800 x 2048 bf16 with residual and checkpoint: 2048 blocks 267 us, 8192
 // 234, 16384 230, 65536 235; 512 columns 61.8, 55.5, 55.5, 55.2), wider ones few
@@ -446,7 +454,8 @@ extern "C" int lrcnn_layer_norm_forward(int64_t rows, int64_t cols, int32_t dtyp
     constexpr int TPR = tpr.value, NV = nv.value, BS = TPR > 256 ? TPR : 256;
     constexpr int R = NV == 1 ? 2 : 1;
     const int64_t per = (int64_t)(BS / TPR) * R;
-    const unsigned g = (unsigned)std::min<int64_t>((rows + per - 1) / per, (NV == 1 ? kFwdBlocks : kFwdBlocksWide) * 256 / BS);
+    const int64_t most = (NV == 1 ? kFwdBlocks : kFwdBlocksWide) * 256 / BS;
+    const unsigned g = (unsigned)std::min<int64_t>((rows + per - 1) / per, most);
     if (dtype == LRCNN_BF16)
       ln_fwd_kernel<bf16, TPR, NV, R><<<g, BS, 0, (hipStream_t)stream>>>(a);
     else
@@ -503,12 +512,18 @@ extern "C" int lrcnn_layer_norm_backward(int64_t rows, int64_t cols, int32_t dty
     a.k = ckpt_of(ckpt, rows, cols);
     by_width((int)cols, [&](auto tpr, auto nv) {
       constexpr int TPR = tpr.value, NV = nv.value, BS = TPR > 256 ? TPR : 256;
-      constexpr int R = NV == 1 ? 4 : 1;
-      const int64_t per = (int64_t)(BS / TPR) * R;
-      parts = (int)std::min<int64_t>((rows + per - 1) / per, kMaxParts);
       auto run = [&](auto *tp, auto ck) {
         using T = std::remove_pointer_t<decltype(tp)>;
-        ln_bwd_kernel<T, ck.value, TPR, NV, R><<<parts, BS, 0, s>>>(a);
+        auto with = [&](auto r) {  // r rows of a group of threads at a time
+          const int64_t per = (int64_t)(BS / TPR) * r.value;
+          parts = (int)std::min<int64_t>((rows + per - 1) / per, kMaxParts);
+          ln_bwd_kernel<T, ck.value, TPR, NV, r.value><<<parts, BS, 0, s>>>(a);
+        };
+        if constexpr (TPR <= 64) {
+          if (rows <= (int64_t)(BS / TPR) * 4 * kFewParts)
+            return with(std::integral_constant<int, 2>());
+        }
+        with(std::integral_constant<int, NV == 1 ? 4 : 1>());
       };
       if (dtype == LRCNN_BF16) {
         if (ckpt) run((bf16 *)nullptr, std::true_type());

@@ -126,12 +126,14 @@ enum Cols {
 // for the ends, 7.6 as here). Columns past the matrix are read from its first
 // ones: what they give is never stored.
 //
-// 67800 x 2048 x 8192 bf16 (2.27 TFLOP) takes 2.08 to 2.15 ms, 1060 to 1093
-// TFLOP/s. The matrix pipes are busy 51% of the cycles and the clock falls to
-// 1.67 GHz: it is bound by power, as this card's own bf16 products are (54%).
-// float32 67800 x 2048 x 2048 takes 1.69 ms: three products, 1009 TFLOP/s.
-// Long and narrow calls (540000 x 64 x 64) are bound by reading dy and the
-// codes; small float32 ones by the instructions that cut dy.
+// 67800 x 2048 x 8192 bf16 (2.27 TFLOP) takes 2.03 to 2.2 ms, 1030 to 1120
+// TFLOP/s: 4.28 million cycles, the matrix pipes busy in 51% of them, at a clock
+// that its own power brings down to 1.7 to 2.0 GHz (2.3 in the small calls); this
+// card's library product of the size runs at 1142 with 54% busy. float32
+// 67800 x 2048 x 2048 takes 1.69 ms, three products, 1009 TFLOP/s. Long and
+// narrow calls (540000 x 256 x 173 bf16: 100 us and 8.9 for the join) are near
+// what reading dy and the codes takes (68 us); small float32 ones (392 x 512 x
+// 2048: 19 us) are bound by the instructions that cut dy, on 64 of the CUs.
 template <typename T, int W, int COLS>
 __global__ __launch_bounds__(256, W == 256 ? 1 : 2) void wgrad8_kernel(WgArgs a) {
   constexpr int P = std::is_same<T, float>::value ? 3 : 1;  // pieces of dy
@@ -297,7 +299,8 @@ __global__ __launch_bounds__(256, W == 256 ? 1 : 2) void wgrad8_kernel(WgArgs a)
   bf16x4 fa[2][NB][2], fb[2][NB][2];
 #pragma unroll
   for (int i = 0; i < 2 * NB; ++i)
-    fa[1][i / 2][i % 2] = fb[1][i / 2][i % 2] = (bf16x4){(__bf16)0.f, (__bf16)0.f, (__bf16)0.f, (__bf16)0.f};
+    fa[1][i / 2][i % 2] = fb[1][i / 2][i % 2] =
+        (bf16x4){(__bf16)0.f, (__bf16)0.f, (__bf16)0.f, (__bf16)0.f};
   float dbv[NB];
 #pragma unroll
   for (int i = 0; i < NB; ++i) dbv[i] = 0.f;
@@ -560,7 +563,7 @@ __global__ __launch_bounds__(256) void wgrad8_join_kernel(WgArgs a, int splits) 
 // 256 bf16 by 3 15.2, 6 12.7, 12 11.3, 24 12.3; 392 x 512 x 2048 bf16 by 1 11.8,
 // 3 17.3, 6 23.4; 784 x 64 x 64 float32 by 1 28.1, 3 17.1, 12 12.2; for the tiles:
 // 67800 x 2048 x 8192 bf16 2784 and 2083, 67800 x 512 x 2048 195 and 188,
-// 540000 x 256 x 256 121 and 130; float32 67800 x 512 x 512 137 and 151 (a
+// 540000 x 256 x 256 117 and 113; float32 67800 x 512 x 512 137 and 151 (a
 // 256-wide float32 tile spills registers and is not kept).
 struct Split {
   int tile, splits;
@@ -687,7 +690,8 @@ extern "C" int lrcnn_linear_wgrad(int64_t rows, int64_t n_in, int64_t n_out, int
     const int64_t nk = n_out * n_in;
     auto join = [&](auto v, auto g) {
       constexpr int E = 256 / g.value * v.value;
-      wgrad8_join_kernel<v.value, g.value><<<(unsigned)((nk + E - 1) / E), 256, 0, s>>>(a, sp.splits);
+      const unsigned blocks = (unsigned)((nk + E - 1) / E);
+      wgrad8_join_kernel<v.value, g.value><<<blocks, 256, 0, s>>>(a, sp.splits);
     };
     auto by_groups = [&](auto v) {
       if (sp.splits <= 8) join(v, std::integral_constant<int, 1>());
