@@ -200,7 +200,7 @@ int by_kind(int32_t kind, F &&f) {
     case LRCNN_ACT_GELU_TANH: return f(std::integral_constant<int, LRCNN_ACT_GELU_TANH>());
     case LRCNN_ACT_SILU: return f(std::integral_constant<int, LRCNN_ACT_SILU>());
   }
-  return lrcnn_fail(LRCNN_EINVAL, "unknown activation");
+  return refuse(LRCNN_EINVAL, "unknown activation");
 }
 
 }  // namespace
@@ -215,7 +215,7 @@ using namespace lrcnn::act8;
   } while (0)
 
 extern "C" int lrcnn_act8_bytes(int64_t rows, int64_t cols, size_t *bytes) {
-  if (!bytes) return lrcnn_fail(LRCNN_EINVAL, "null output");
+  if (!bytes) return refuse(LRCNN_EINVAL, "null output");
   TRY(take_shape(rows, cols, LRCNN_F32));
   *bytes = ckpt_bytes(rows, cols);
   return LRCNN_OK;
@@ -267,11 +267,11 @@ extern "C" int lrcnn_activation_forward(int64_t rows, int64_t cols, int32_t dtyp
   TRY(take_shape(rows, cols, dtype));
   const int es = dtype == LRCNN_BF16 ? 2 : 4;
   if (kind < LRCNN_ACT_RELU || kind > LRCNN_ACT_SILU)
-    return lrcnn_fail(LRCNN_EINVAL, "unknown activation");
-  if (ckpt_v && !v) return lrcnn_fail(LRCNN_EINVAL, "ckpt_v without v");
+    return refuse(LRCNN_EINVAL, "unknown activation");
+  if (ckpt_v && !v) return refuse(LRCNN_EINVAL, "ckpt_v without v");
   if (rows == 0) return LRCNN_OK;
   if (!a && !ckpt_u && !ckpt_v && !ckpt_a)
-    return lrcnn_fail(LRCNN_EINVAL, "activation_forward: no output");
+    return refuse(LRCNN_EINVAL, "activation_forward: no output");
   Mat m[3];  // u, v, a
   TRY(take("u", u, ldu, cols, es, true, &m[0]));
   TRY(take("v", v, ldv, cols, es, false, &m[1]));
@@ -308,12 +308,12 @@ extern "C" int lrcnn_activation_backward(int64_t rows, int64_t cols, int32_t dty
   TRY(take_shape(rows, cols, dtype));
   const int es = dtype == LRCNN_BF16 ? 2 : 4;
   if (kind < LRCNN_ACT_RELU || kind > LRCNN_ACT_SILU)
-    return lrcnn_fail(LRCNN_EINVAL, "unknown activation");
+    return refuse(LRCNN_EINVAL, "unknown activation");
   const bool ck = ckpt_u != nullptr, gated = v || ckpt_v;
   if (rows == 0) return LRCNN_OK;
   if ((u != nullptr) == ck || (gated && ((ckpt_v != nullptr) != ck || (v != nullptr) == ck)))
-    return lrcnn_fail(LRCNN_EINVAL, "give u (and v) either full-width or as checkpoints");
-  if (gated != (dv != nullptr)) return lrcnn_fail(LRCNN_EINVAL, "dv goes with v or ckpt_v");
+    return refuse(LRCNN_EINVAL, "give u (and v) either full-width or as checkpoints");
+  if (gated != (dv != nullptr)) return refuse(LRCNN_EINVAL, "dv goes with v or ckpt_v");
   Mat m[5];  // da, u, v, du, dv
   TRY(take("da", da, ldda, cols, es, true, &m[0]));
   TRY(take("u", u, ldu, cols, es, false, &m[1]));

@@ -55,6 +55,23 @@ inline Ckpt ckpt_of(const void *p, int64_t rows, int64_t cols) {
 }
 
 // ------------------------------------------------------ argument checks
+// The code of a refusal, its message kept; no exception (memory for the message)
+// leaves a C entry.
+inline void put_part(std::string &m, const char *p) { m += p; }
+template <typename N>
+void put_part(std::string &m, N n) {
+  m += std::to_string(n);
+}
+template <typename... P>
+int refuse(int code, P... parts) noexcept {
+  try {
+    std::string m;
+    (put_part(m, parts), ...);
+    return lrcnn_fail(code, m);
+  } catch (...) {
+    return code;
+  }
+}
 // A row-major matrix of the caller: rows at `ld` elements from each other
 // (0: dense). Any alignment of a whole element will do.
 struct Mat {
@@ -65,39 +82,39 @@ struct Mat {
 // pointer that cuts an element, or rows that overlap.
 inline int take(const char *what, const void *p, int64_t ld, int64_t cols, int es, bool must,
                 Mat *m) {
-  if (!p && must) return lrcnn_fail(LRCNN_EINVAL, std::string(what) + " is null");
-  if ((uintptr_t)p % es) return lrcnn_fail(LRCNN_EINVAL, std::string(what) + " is misaligned");
+  if (!p && must) return refuse(LRCNN_EINVAL, what, " is null");
+  if ((uintptr_t)p % es) return refuse(LRCNN_EINVAL, what, " is misaligned");
   if (p && ld != 0 && ld < cols)
-    return lrcnn_fail(LRCNN_ESHAPE, std::string(what) + ": row stride smaller than a row");
+    return refuse(LRCNN_ESHAPE, what, ": row stride smaller than a row");
   if (p && ld > ((int64_t)1 << 40))
-    return lrcnn_fail(LRCNN_ESHAPE, std::string(what) + ": row stride too large");
+    return refuse(LRCNN_ESHAPE, what, ": row stride too large");
   m->p = (char *)p;
   m->ld = ld ? ld : cols;
   return LRCNN_OK;
 }
 inline int take_f32(const char *what, const void *p, bool must) {
-  if (!p && must) return lrcnn_fail(LRCNN_EINVAL, std::string(what) + " is null");
-  if ((uintptr_t)p & 3) return lrcnn_fail(LRCNN_EINVAL, std::string(what) + " is misaligned");
+  if (!p && must) return refuse(LRCNN_EINVAL, what, " is null");
+  if ((uintptr_t)p & 3) return refuse(LRCNN_EINVAL, what, " is misaligned");
   return LRCNN_OK;
 }
 inline int take_ckpt(const char *what, const void *p, bool must) {
-  if (!p && must) return lrcnn_fail(LRCNN_EINVAL, std::string(what) + " is null");
+  if (!p && must) return refuse(LRCNN_EINVAL, what, " is null");
   if ((uintptr_t)p & 15)
-    return lrcnn_fail(LRCNN_EINVAL, std::string(what) + " is not 16-byte aligned");
+    return refuse(LRCNN_EINVAL, what, " is not 16-byte aligned");
   return LRCNN_OK;
 }
 inline int take_shape(int64_t rows, int64_t cols, int32_t dtype) {
   if (dtype != LRCNN_F32 && dtype != LRCNN_BF16)
-    return lrcnn_fail(LRCNN_EDTYPE, "dtype must be LRCNN_F32 or LRCNN_BF16");
-  if (rows < 0 || cols < 1) return lrcnn_fail(LRCNN_ESHAPE, "need rows >= 0 and cols >= 1");
+    return refuse(LRCNN_EDTYPE, "dtype must be LRCNN_F32 or LRCNN_BF16");
+  if (rows < 0 || cols < 1) return refuse(LRCNN_ESHAPE, "need rows >= 0 and cols >= 1");
   if (rows > kMaxRows || cols > kMaxCols || (rows && cols > kMaxElems / rows))
-    return lrcnn_fail(LRCNN_ESHAPE, "matrix too large");
+    return refuse(LRCNN_ESHAPE, "matrix too large");
   return LRCNN_OK;
 }
 inline int launched(const char *what) {
   const hipError_t e = hipGetLastError();
   if (e == hipSuccess) return LRCNN_OK;
-  return lrcnn_fail(LRCNN_EHIP, std::string(what) + ": " + hipGetErrorString(e));
+  return refuse(LRCNN_EHIP, what, ": ", hipGetErrorString(e));
 }
 
 #ifdef __HIPCC__

@@ -409,8 +409,7 @@ int norm_shape(int64_t rows, int64_t cols, int32_t dtype) {
   const int st = take_shape(rows, cols, dtype);
   if (st != LRCNN_OK) return st;
   if (cols > kMaxNormCols)
-    return lrcnn_fail(LRCNN_ESHAPE, "layer norm takes at most " + std::to_string(kMaxNormCols) +
-                                        " columns");
+    return refuse(LRCNN_ESHAPE, "layer norm takes at most ", kMaxNormCols, " columns");
   return LRCNN_OK;
 }
 
@@ -432,8 +431,8 @@ extern "C" int lrcnn_layer_norm_forward(int64_t rows, int64_t cols, int32_t dtyp
                                         float *mean, float *rstd, void *ckpt, void *stream) {
   TRY(norm_shape(rows, cols, dtype));
   if (!(eps >= 0.f) || !(eps < INFINITY))
-    return lrcnn_fail(LRCNN_EINVAL, "eps must be finite and not negative");
-  if (total && !residual) return lrcnn_fail(LRCNN_EINVAL, "total goes with residual");
+    return refuse(LRCNN_EINVAL, "eps must be finite and not negative");
+  if (total && !residual) return refuse(LRCNN_EINVAL, "total goes with residual");
   if (rows == 0) return LRCNN_OK;
   const int es = dtype == LRCNN_BF16 ? 2 : 4;
   FwdArgs a{};
@@ -465,7 +464,7 @@ extern "C" int lrcnn_layer_norm_forward(int64_t rows, int64_t cols, int32_t dtyp
 }
 
 extern "C" int lrcnn_layer_norm_workspace_bytes(int64_t rows, int64_t cols, size_t *bytes) {
-  if (!bytes) return lrcnn_fail(LRCNN_EINVAL, "null output");
+  if (!bytes) return refuse(LRCNN_EINVAL, "null output");
   TRY(norm_shape(rows, cols, LRCNN_F32));
   *bytes = a256((size_t)parts_of(rows) * 2 * (size_t)cols * 4);
   return LRCNN_OK;
@@ -486,7 +485,7 @@ extern "C" int lrcnn_layer_norm_backward(int64_t rows, int64_t cols, int32_t dty
   const bool grads = dgamma || dbeta;
   if (rows) {
     if ((x != nullptr) == (ckpt != nullptr) || (x != nullptr) != (mean != nullptr))
-      return lrcnn_fail(LRCNN_EINVAL, "give x with mean, or ckpt");
+      return refuse(LRCNN_EINVAL, "give x with mean, or ckpt");
     TRY(take("dy", dy, lddy, cols, es, true, &a.dy));
     TRY(take("x", x, ldx, cols, es, false, &a.x));
     TRY(take("dres", dres, lddr, cols, es, false, &a.dres));
@@ -498,10 +497,9 @@ extern "C" int lrcnn_layer_norm_backward(int64_t rows, int64_t cols, int32_t dty
   }
   const size_t need = a256((size_t)parts_of(rows) * 2 * (size_t)cols * 4);
   if (grads && (!workspace || ((uintptr_t)workspace & 15)))
-    return lrcnn_fail(LRCNN_EINVAL, "workspace null or misaligned");
+    return refuse(LRCNN_EINVAL, "workspace null or misaligned");
   if (grads && ws_bytes < need)
-    return lrcnn_fail(LRCNN_EWORKSPACE, "workspace needs " + std::to_string(need) +
-                                            " bytes, got " + std::to_string(ws_bytes));
+    return refuse(LRCNN_EWORKSPACE, "workspace needs ", need, " bytes, got ", ws_bytes);
   hipStream_t s = (hipStream_t)stream;
   int parts = 0;
   if (rows) {

@@ -599,9 +599,9 @@ int wgrad_shape(int64_t rows, int64_t n_in, int64_t n_out, int32_t dtype) {
   if (st == LRCNN_OK) st = take_shape(rows, n_out, dtype);
   if (st == LRCNN_OK) st = take_shape(n_out, n_in, dtype);
   if (st == LRCNN_OK && (n_in > kMaxFeatures || n_out > kMaxFeatures))
-    st = lrcnn_fail(LRCNN_ESHAPE, "more than 2^24 features");
+    st = refuse(LRCNN_ESHAPE, "more than 2^24 features");
   if (st == LRCNN_OK && rows > kMaxWgradRows)
-    st = lrcnn_fail(LRCNN_ESHAPE, "weight gradient over more than 2^30 rows");
+    st = refuse(LRCNN_ESHAPE, "weight gradient over more than 2^30 rows");
   return st;
 }
 
@@ -618,7 +618,7 @@ using namespace lrcnn::act8;
 
 extern "C" int lrcnn_linear_wgrad_workspace_bytes(int64_t rows, int64_t n_in, int64_t n_out,
                                                   int32_t dtype, size_t *bytes) {
-  if (!bytes) return lrcnn_fail(LRCNN_EINVAL, "null output");
+  if (!bytes) return refuse(LRCNN_EINVAL, "null output");
   TRY(wgrad_shape(rows, n_in, n_out, dtype));
   *bytes = wgrad_ws(split_of(rows, n_out, n_in, dtype), n_out, n_in);
   return LRCNN_OK;
@@ -633,7 +633,7 @@ extern "C" int lrcnn_linear_wgrad(int64_t rows, int64_t n_in, int64_t n_out, int
   WgArgs a{};
   TRY(take("dy", dy, lddy, n_out, dtype == LRCNN_BF16 ? 2 : 4, rows > 0, &a.dy));
   if (rows > 0 && a.dy.ld > kMaxFeatures)
-    return lrcnn_fail(LRCNN_ESHAPE, "dy: row stride of more than 2^24");
+    return refuse(LRCNN_ESHAPE, "dy: row stride of more than 2^24");
   TRY(take_ckpt("ckpt", ckpt, rows > 0));
   TRY(take_f32("scale", scale, false));
   TRY(take_f32("shift", shift, false));
@@ -642,10 +642,9 @@ extern "C" int lrcnn_linear_wgrad(int64_t rows, int64_t n_in, int64_t n_out, int
   const Split sp = split_of(rows, n_out, n_in, dtype);
   const size_t need = wgrad_ws(sp, n_out, n_in);
   if (need && (!workspace || ((uintptr_t)workspace & 15)))
-    return lrcnn_fail(LRCNN_EINVAL, "workspace null or misaligned");
+    return refuse(LRCNN_EINVAL, "workspace null or misaligned");
   if (ws_bytes < need)
-    return lrcnn_fail(LRCNN_EWORKSPACE, "workspace needs " + std::to_string(need) +
-                                            " bytes, got " + std::to_string(ws_bytes));
+    return refuse(LRCNN_EWORKSPACE, "workspace needs ", need, " bytes, got ", ws_bytes);
   a.rows = (int)rows, a.n = (int)n_out, a.k = (int)n_in, a.splits = sp.splits;
   a.q = ckpt_of(ckpt, rows, n_in);
   a.q.pitch = pitch_of(n_in);
@@ -655,7 +654,7 @@ extern "C" int lrcnn_linear_wgrad(int64_t rows, int64_t n_in, int64_t n_out, int
     a.dbpart = (float *)((char *)workspace + a256((size_t)sp.splits * n_out * n_in * 4));
   }
   const int64_t gx = (n_out + sp.tile - 1) / sp.tile, gy = (n_in + sp.tile - 1) / sp.tile;
-  if (gx * gy * sp.splits >= (1 << 24)) return lrcnn_fail(LRCNN_ESHAPE, "too many features");
+  if (gx * gy * sp.splits >= (1 << 24)) return refuse(LRCNN_ESHAPE, "too many features");
   a.gx = (int)gx, a.gy = (int)gy;
   a.tiles = lrcnn::fast_div((uint32_t)(gx * gy));
   a.panel = lrcnn::fast_div((uint32_t)(8 * gy));
