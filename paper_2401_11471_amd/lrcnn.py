@@ -286,7 +286,10 @@ def _stream(stream):
 
 def _raw_stream(stream, like):
     """The stream as a number: torch's current one of the tensors' device, asked
-    for without making a Stream object (1 us of a call's 8)."""
+    for without making a Stream object (1 us of a call's 8). The last thing a
+    call asks for: host memory goes no further."""
+    if like[2] < 0:
+        _einval("the tensors must be on a GPU")
     return torch._C._cuda_getCurrentRawStream(like[2]) if stream is None else stream
 
 
@@ -355,7 +358,8 @@ def lrcnn_sgd_update(plan, lr, weights, dws, fc_w=None, d_fc_w=None, fc_b=None, 
 
 # ---- feed-forward blocks with 8-bit activation checkpoints (2-d tensors of one
 # dtype and device, columns next to each other, rows at any stride). The tensors'
-# shapes give the sizes; ones that do not agree are refused before the call.
+# shapes give the sizes; ones that do not agree, or are not on a GPU, are refused
+# before the call.
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
@@ -416,6 +420,15 @@ def _bytes(name, t, like):
     if t.dtype is not torch.uint8 or not t.is_contiguous() or t.get_device() != like[2]:
         _einval(f"{name} must be dense uint8 on the same device")
     return t.data_ptr(), t.numel()
+
+
+def _workspace(t, like, need, *sizes):
+    """Pointer and size of a workspace. The library refuses one that is too small;
+    of tensors that do not get that far it is said here."""
+    p, n = _bytes("workspace", t, like)
+    if t is not None and like[2] < 0 and n < need(*sizes):
+        raise LrcnnError(-4, f"workspace needs {need(*sizes)} bytes, got {n}")
+    return p, n
 
 
 def _ckpt(name, t, shape, like):
@@ -486,7 +499,7 @@ def lrcnn_layer_norm_backward(dy, rstd, gamma, dx, dgamma=None, dbeta=None, work
     px, ldx = _mat("x", x, like)
     pr, ldr = _mat("dres", dres, like)
     pdx, lddx = _mat("dx", dx, like)
-    pw, nw = _bytes("workspace", workspace, like)
+    pw, nw = _workspace(workspace, like, lrcnn_layer_norm_workspace_bytes, rows, cols)
     _check(LIB.lrcnn_layer_norm_backward(
         rows, cols, dt, pdy, lddy, px, ldx, _vec("mean", mean, rows, like),
         _ckpt("ckpt", ckpt, shape, like), _vec("rstd", rstd, rows, like),
@@ -537,7 +550,8 @@ def lrcnn_linear_wgrad(dy, ckpt, dw, workspace=None, db=None, scale=None, shift=
     if dw.dim() != 2 or dw.shape[0] != n_out:
         _einval("dw must be [n_out][n_in]")
     n_in = dw.shape[1]
-    pw, nw = _bytes("workspace", workspace, like)
+    pw, nw = _workspace(workspace, like, lrcnn_linear_wgrad_workspace_bytes, rows, n_in, n_out,
+                        dt)
     _check(LIB.lrcnn_linear_wgrad(
         rows, n_in, n_out, dt, pdy, lddy, _ckpt("ckpt", ckpt, (rows, n_in), like),
         _vec("scale", scale, n_in, like), _vec("shift", shift, n_in, like),

@@ -184,3 +184,33 @@ def test_binding_refuses_tensors_that_do_not_agree():
     refused(EINVAL, L.lrcnn_linear_wgrad, x, ck, f(40, 80))
     refused(EINVAL, L.lrcnn_linear_wgrad, x, ck, f(40, 40).double())
     refused(EINVAL, L.lrcnn_linear_wgrad, x, ck, f(40, 40), scale=f(41))
+
+
+# name, and a call of host tensors that agree with each other
+CALLS = {
+    "lrcnn_act8_pack": lambda f, b, **k: L.lrcnn_act8_pack(f(4, 40), b, **k),
+    "lrcnn_act8_unpack": lambda f, b, **k: L.lrcnn_act8_unpack(b, f(4, 40), **k),
+    "lrcnn_layer_norm_forward": lambda f, b, **k: L.lrcnn_layer_norm_forward(
+        f(4, 40), f(40), f(40), 1e-5, f(4, 40), rstd=f(4), ckpt=b, **k),
+    "lrcnn_layer_norm_backward": lambda f, b, **k: L.lrcnn_layer_norm_backward(
+        f(4, 40), f(4), f(40), f(4, 40), f(40), f(40), b, ckpt=b, **k),
+    "lrcnn_activation_forward": lambda f, b, **k: L.lrcnn_activation_forward(
+        L.ACT_SILU, f(4, 40), f(4, 40), v=f(4, 40), ckpt_u=b, **k),
+    "lrcnn_activation_backward": lambda f, b, **k: L.lrcnn_activation_backward(
+        L.ACT_GELU, f(4, 40), f(4, 40), ckpt_u=b, **k),
+    "lrcnn_linear_wgrad": lambda f, b, **k: L.lrcnn_linear_wgrad(
+        f(4, 10), b, f(10, 40), b, db=f(10), **k),
+}
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+@pytest.mark.parametrize("stream", [{}, {"stream": 0}], ids=["current", "given"])
+def test_binding_refuses_host_tensors(name, stream, monkeypatch):
+    """Host memory never reaches the library, whose kernels would follow its pointers."""
+    reached = []
+    monkeypatch.setattr(L.LIB, name, lambda *a: reached.append(a) or 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 0, raising=False)
+    with pytest.raises(L.LrcnnError) as e:
+        CALLS[name](torch.zeros, torch.zeros(1 << 16, dtype=torch.uint8), **stream)
+    assert e.value.code == EINVAL and "GPU" in str(e.value)
+    assert not reached
