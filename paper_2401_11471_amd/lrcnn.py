@@ -287,10 +287,14 @@ def _stream(stream):
 def _raw_stream(stream, like):
     """The stream as a number: torch's current one of the tensors' device, asked
     for without making a Stream object (1 us of a call's 8). The last thing a
-    call asks for: host memory goes no further."""
-    if like[2] < 0:
+    call asks for: neither host memory goes further nor another GPU's. (Launches
+    go to the current device, and the default stream is 0 on each.)"""
+    dev = like[2]
+    if dev < 0:
         _einval("the tensors must be on a GPU")
-    return torch._C._cuda_getCurrentRawStream(like[2]) if stream is None else stream
+    if dev != torch._C._cuda_getDevice():
+        _einval(f"the tensors are on cuda:{dev}, which is not the current device")
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream
 
 
 def lrcnn_forward_rows(plan, x, weights, scales, shifts, y, workspace, masks=None,
@@ -358,8 +362,8 @@ def lrcnn_sgd_update(plan, lr, weights, dws, fc_w=None, d_fc_w=None, fc_b=None, 
 
 # ---- feed-forward blocks with 8-bit activation checkpoints (2-d tensors of one
 # dtype and device, columns next to each other, rows at any stride). The tensors'
-# shapes give the sizes; ones that do not agree, or are not on a GPU, are refused
-# before the call.
+# shapes give the sizes; ones that do not agree, or are not on the current GPU, are
+# refused before the call.
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 

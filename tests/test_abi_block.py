@@ -214,3 +214,22 @@ def test_binding_refuses_host_tensors(name, stream, monkeypatch):
         CALLS[name](torch.zeros, torch.zeros(1 << 16, dtype=torch.uint8), **stream)
     assert e.value.code == EINVAL and "GPU" in str(e.value)
     assert not reached
+
+
+@pytest.mark.parametrize("stream", [None, 0, 77])
+def test_binding_refuses_tensors_of_another_gpu(stream, monkeypatch):
+    """Tensors of GPU 1 are worked on while it is current, in its stream, and refused
+    while GPU 0 is: the library launches on the current device."""
+    calls = []
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 100 + dev, raising=False)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 1)
+    for name, call in CALLS.items():
+        monkeypatch.setattr(L.LIB, name, lambda *a: calls.append(a[-1]) or 0)
+        run = lambda: call(torch.zeros, torch.zeros(1 << 16, dtype=torch.uint8), stream=stream)
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+        with pytest.raises(L.LrcnnError) as e:
+            run()
+        assert e.value.code == EINVAL and "cuda:1" in str(e.value) and not calls
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
+        run()
+        assert calls.pop() == (101 if stream is None else stream) and not calls
