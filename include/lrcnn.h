@@ -453,7 +453,9 @@ int lrcnn_activation_backward(int64_t rows, int64_t cols, int32_t dtype,
                               void *dv, int64_t lddv, void *ckpt_a,
                               void *stream);
 
-/* Device scratch bytes of lrcnn_linear_wgrad (0: none, NULL will do). */
+/* Device scratch bytes of lrcnn_linear_wgrad for up to `rows` rows (0: none,
+ * NULL will do). Never less than for fewer rows: the workspace of the largest
+ * band or micro-batch serves all of them. */
 int lrcnn_linear_wgrad_workspace_bytes(int64_t rows, int64_t n_in,
                                        int64_t n_out, int32_t dtype,
                                        size_t *bytes);

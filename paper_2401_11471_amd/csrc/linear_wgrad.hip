@@ -565,33 +565,67 @@ __global__ __launch_bounds__(256) void wgrad8_join_kernel(WgArgs a, int splits) 
 // 67800 x 2048 x 8192 bf16 2784 and 2083, 67800 x 512 x 2048 195 and 188,
 // 540000 x 256 x 256 117 and 113; float32 67800 x 512 x 512 137 and 151 (a
 // 256-wide float32 tile spills registers and is not kept).
+//
+// The choice goes up and down with the rows, so a workspace that serves any
+// smaller number of rows too is one for `most` splits: the largest count that
+// can be chosen for these rows or fewer. At t <= steps a count s takes at least
+// t p / s + d, p a step's time over all of a CU's workgroups and d what the
+// split costs. So it is never chosen if steps (p1 - p / s) < d, with p1 the p of
+// one split, nor if the count that fills the CUs once or twice, at most
+// t p' / s' + p' + d', is always less.
 struct Split {
-  int tile, splits;
+  int tile, splits, most;
 };
 Split split_of(int64_t rows, int64_t n, int64_t k, int32_t dtype) {
   const int64_t steps = (rows + kStep - 1) / kStep;
-  Split best{128, 1};
+  Split best{128, 1, 1};
   double least_us = -1;
-  // (of a 256-wide tile half would be empty at 128 columns or fewer)
-  const int widest = dtype == LRCNN_BF16 && n > 128 && k > 128 ? 256 : 128;
-  for (int tile = 128; tile <= widest; tile *= 2) {
-    const int64_t tiles = ((n + tile - 1) / tile) * ((k + tile - 1) / tile);
-    const double step_us = tile == 256 ? 0.98 : dtype == LRCNN_BF16 ? 0.35 : 0.82;
-    auto consider = [&](int64_t s) {
-      if (s < 1 || (s > 1 && (s > steps || s * tiles > 1024))) return;
+  struct Rate {
+    int64_t tiles;
+    double step_us;
+    int tile;
+    double p(int64_t s, int64_t times = 1) const {
       const double per_cu = (double)((tiles * s + 255) / 256);
-      const double share = tile == 128 && per_cu > 1 ? 0.85 : 1.0;
-      double us = (double)((steps + s - 1) / s) * step_us * per_cu * share;
-      if (s > 1) us += 2.5 + 2.2e-6 * (double)s * (double)n * (double)k;
-      if (least_us < 0 || us < least_us) least_us = us, best = Split{tile, (int)s};
+      return (double)times * step_us * per_cu * (tile == 128 && per_cu > 1 ? 0.85 : 1.0);
+    }
+  } rate[2];
+  auto d = [&](int64_t s) {
+    return s > 1 ? 2.5 + 2.2e-6 * (double)s * (double)n * (double)k : 0.0;
+  };
+  // (of a 256-wide tile half would be empty at 128 columns or fewer)
+  const int widths = dtype == LRCNN_BF16 && n > 128 && k > 128 ? 2 : 1;
+  double p1 = 0;
+  for (int i = 0; i < widths; ++i) {
+    const int tile = 128 << i;
+    rate[i].tile = tile;
+    rate[i].tiles = ((n + tile - 1) / tile) * ((k + tile - 1) / tile);
+    rate[i].step_us = tile == 256 ? 0.98 : dtype == LRCNN_BF16 ? 0.35 : 0.82;
+    p1 = i ? std::min(p1, rate[i].p(1)) : rate[i].p(1);
+  }
+  auto never = [&](int64_t s, double p) {
+    if ((double)steps * (p1 - p / (double)s) < d(s) - 1e-6) return true;
+    for (int i = 0; i < widths; ++i)
+      for (const int64_t f : {256 / rate[i].tiles, 512 / rate[i].tiles})
+        if (f >= 1 && f < s && p * (double)f >= rate[i].p(f) * (double)s &&
+            rate[i].p(f) + d(f) <= d(s))
+          return true;
+    return false;
+  };
+  for (int i = 0; i < widths; ++i) {
+    const Rate &r = rate[i];
+    auto consider = [&](int64_t s) {
+      if (s < 1 || (s > 1 && (s > steps || s * r.tiles > 1024))) return;
+      const double us = r.p(s, (steps + s - 1) / s) + d(s);
+      if (least_us < 0 || us < least_us) least_us = us, best.tile = r.tile, best.splits = (int)s;
+      if (s > best.most && !never(s, r.p(s))) best.most = (int)s;
     };
     for (int64_t s = 1; s <= 512; s += s < 8 ? 1 : s / 4) consider(s);
-    consider(256 / tiles), consider(512 / tiles);  // one or two workgroups on every CU
+    consider(256 / r.tiles), consider(512 / r.tiles);  // one or two workgroups on every CU
   }
   return best;
 }
-size_t wgrad_ws(const Split &s, int64_t n, int64_t k) {
-  return s.splits == 1 ? 0 : a256((size_t)s.splits * n * k * 4) + a256((size_t)s.splits * n * 4);
+size_t wgrad_ws(int64_t splits, int64_t n, int64_t k) {
+  return splits == 1 ? 0 : a256((size_t)splits * n * k * 4) + a256((size_t)splits * n * 4);
 }
 
 int wgrad_shape(int64_t rows, int64_t n_in, int64_t n_out, int32_t dtype) {
@@ -620,7 +654,7 @@ extern "C" int lrcnn_linear_wgrad_workspace_bytes(int64_t rows, int64_t n_in, in
                                                   int32_t dtype, size_t *bytes) {
   if (!bytes) return refuse(LRCNN_EINVAL, "null output");
   TRY(wgrad_shape(rows, n_in, n_out, dtype));
-  *bytes = wgrad_ws(split_of(rows, n_out, n_in, dtype), n_out, n_in);
+  *bytes = wgrad_ws(split_of(rows, n_out, n_in, dtype).most, n_out, n_in);
   return LRCNN_OK;
 }
 
@@ -640,7 +674,7 @@ extern "C" int lrcnn_linear_wgrad(int64_t rows, int64_t n_in, int64_t n_out, int
   TRY(take_f32("dw", dw, true));
   TRY(take_f32("db", db, false));
   const Split sp = split_of(rows, n_out, n_in, dtype);
-  const size_t need = wgrad_ws(sp, n_out, n_in);
+  const size_t need = sp.splits == 1 ? 0 : wgrad_ws(sp.most, n_out, n_in);
   if (need && (!workspace || ((uintptr_t)workspace & 15)))
     return refuse(LRCNN_EINVAL, "workspace null or misaligned");
   if (ws_bytes < need)

@@ -233,3 +233,25 @@ def test_binding_refuses_tensors_of_another_gpu(stream, monkeypatch):
         monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
         run()
         assert calls.pop() == (101 if stream is None else stream) and not calls
+
+
+@pytest.mark.parametrize("n_in,n_out,dtype,last", [
+    (2048, 2048, L.BF16, 67800), (512, 512, L.BF16, 6400), (256, 173, L.BF16, 540000),
+    (64, 64, L.F32, 16000), (512, 2048, L.F32, 4000), (2048, 8192, L.BF16, 67800),
+    (515, 300, L.F32, 30000), (33, 7, L.BF16, 30000), (300, 3000, L.BF16, 9000)])
+def test_linear_wgrad_workspace_serves_fewer_rows(n_in, n_out, dtype, last):
+    """The workspace of the largest band or micro-batch is enough for all: it never
+    shrinks as the rows grow, and stays within what two (128 x 128) or one
+    (256 x 256) float32 tiles a CU take."""
+    need = [L.lrcnn_linear_wgrad_workspace_bytes(r, n_in, n_out, dtype)
+            for r in range(0, last, max(1, last // 3000))]
+    assert need == sorted(need)
+    assert need[0] == 0 and need[-1] <= 256 * 256 * 256 * 4 + 256 * n_out * 4 + 512
+
+
+def test_linear_wgrad_takes_the_workspace_it_asks_for():
+    """A split weight gradient refuses anything less, also where a call of these
+    rows alone would fit."""
+    for rows in range(32 * 100, 32 * 200, 37):
+        need = L.lrcnn_linear_wgrad_workspace_bytes(rows, 64, 64)
+        assert wgrad(rows=rows, ws_bytes=need - 1) == EWORKSPACE and str(need) in last()

@@ -619,3 +619,29 @@ def test_linear_wgrad_wide(rows, n_in, n_out, dtype, affine):
 def test_linear_wgrad_few_outputs_of_many_inputs(dtype):
     for n_out in (1, 7, 9):
         test_linear_wgrad(40, 70001, n_out, dtype, True)
+
+
+def test_linear_wgrad_bands_share_a_workspace():
+    """Bands of falling height, summed with `accumulate`, in the workspace of the
+    first one; the choice of splits goes up and down on the way. Nothing is
+    written behind it."""
+    n_in, n_out, bands = 512, 512, (672, 640, 353, 32, 1)
+    tell("wgrad bands", bands)
+    rng = np.random.default_rng(5)
+    need = L.lrcnn_linear_wgrad_workspace_bytes(bands[0], n_in, n_out, L.BF16)
+    assert need > 0
+    whole = buf(need + 4096)
+    ws = whole[:need]
+    dw, db = torch.full((n_out, n_in), 9.0, device="cuda"), torch.full((n_out,), 9.0, device="cuda")
+    rw = rb = tw = tb = 0
+    for i, rows in enumerate(bands):
+        c, q = checkpoint_of(features(rng, rows, n_in))
+        dy = matrix(rng.standard_normal((rows, n_out)), BF16)
+        L.lrcnn_linear_wgrad(dy, c, dw, ws, db=db, accumulate=i > 0)
+        w, b = OB.linear_wgrad(np64(dy), q)
+        rw, rb = rw + w, rb + b
+        w, b = OB.linear_wgrad(np.abs(np64(dy)), np.abs(q))
+        tw, tb = tw + w, tb + b
+    close(dw, rw, 1e-5 * tw)
+    close(db, rb, 1e-5 * tb)
+    assert (whole[need:] == 0xA5).all()
