@@ -645,3 +645,44 @@ def test_linear_wgrad_bands_share_a_workspace():
     close(dw, rw, 1e-5 * tw)
     close(db, rb, 1e-5 * tb)
     assert (whole[need:] == 0xA5).all()
+
+
+@pytest.mark.parametrize("rows,cols,value", [
+    (3, 64, 0.1), (5, 512, 0.1), (70, 96, 0.3), (9, 96, 100.7), (2, 31, -33.3), (4, 1000, 1e-3),
+    (3, 2048, 12345.678), (2, 5000, 0.7), (2, 16384, -1e6 / 3)])
+def test_layer_norm_of_constant_float32_rows(rows, cols, value):
+    """A row of one value has that value as its mean, whatever the rounding of
+    its sum, and nothing is left of it but beta: d = v - mean is a few ulps of v,
+    a small whole number of them, so its sum and quotient are exact."""
+    t = torch.full((rows, cols), value, device="cuda")
+    be = torch.randn(cols, device="cuda", generator=torch.Generator("cuda").manual_seed(cols))
+    y, c = torch.empty_like(t), ckpt(rows, cols)
+    mean, rstd = vec(np.zeros(rows)), vec(np.zeros(rows))
+    L.lrcnn_layer_norm_forward(t, None, be, 1e-5, y, mean=mean, rstd=rstd, ckpt=c)
+    assert torch.equal(mean, t[:, 0])
+    assert torch.equal(y, be.expand(rows, cols))
+    # the variance, (d^2) summed less the mean's correction squared: off by 64 u
+    # of d^2, d within 64 u of the value
+    slack = 64 * 2.0 ** -24 * (64 * 2.0 ** -24 * value) ** 2
+    assert np.allclose(np64(rstd), 1e-5 ** -0.5, rtol=1e-6 + slack / 2e-5, atol=0)
+    h = torch.empty_like(t)
+    L.lrcnn_act8_unpack(c, h)
+    assert (h == 0).all()
+
+
+@pytest.mark.parametrize("cols", [96, 500, 2048, 5000])
+def test_layer_norm_far_from_zero(cols):
+    """Rows whose mean is 10^4 times their spread: the mean is its float32 value,
+    half an ulp off, and the normalised rows carry no more than that plus their
+    own 64 u, not the rounding of a sum of large values."""
+    rng = np.random.default_rng(cols)
+    x = np64(vec(1e4 + rng.standard_normal((40, cols))))
+    y, mean, rstd = torch.empty(40, cols, device="cuda"), vec(np.zeros(40)), vec(np.zeros(40))
+    L.lrcnn_layer_norm_forward(vec(x), None, None, 1e-5, y, mean=mean, rstd=rstd)
+    ry, xh, rm, rr = OB.layer_norm(x, np.ones(cols), 0, 1e-5)
+    close(mean, rm, 2.0 ** -24 * np.abs(rm))
+    close(rstd, rr, 4e-6 * rr)
+    # x - mean0 is exact or off by half its ulp; the correction by 64 u of
+    # the mean0's error, itself within 64 u of the mean
+    slack = 64 * 2.0 ** -24 * 64 * 2.0 ** -24 * np.abs(rm[:, None])
+    close(y, ry, rr[:, None] * slack + 4e-6 * (1 + np.abs(ry)))
