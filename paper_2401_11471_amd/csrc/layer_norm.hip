@@ -101,6 +101,18 @@ __device__ __forceinline__ void row_sums(float (&s)[N], float *red, int &turn) {
   }
 }
 
+// 1 / sqrt(x) to the last bit but for near ties: the instruction's value, an ulp off
+// in one row of seven (an error that a whole row and its checkpoint share), and
+// one Newton step y + y (1 - x y^2) / 2, x y as a sum of two floats. Zero and
+// infinity, where the step is NaN, keep their limits.
+__device__ __forceinline__ float rsqrt_rounded(float x) {
+  const float y = rsqrtf(x);
+  const float h = x * y, l = fmaf(x, y, -h);
+  const float e = fmaf(-l, y, fmaf(-h, y, 1.f));
+  const float z = fmaf(0.5f * e, y, y);
+  return z == z ? z : y;
+}
+
 struct FwdArgs {
   int64_t rows;
   int cols, pitch;
@@ -206,7 +218,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void ln_fwd_kernel(FwdArgs a
         var -= off * off;
         var = var < 0.f ? 0.f : var;  // (NaN stays)
       }
-      const float rs = rsqrtf(var + a.eps);
+      const float rs = rsqrt_rounded(var + a.eps);
       if (r0 + sub * R + q >= a.rows) continue;
       if (t == 0) {
         if (a.mean) a.mean[row[q]] = mu[q];

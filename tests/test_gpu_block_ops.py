@@ -686,3 +686,25 @@ def test_layer_norm_far_from_zero(cols):
     # the mean0's error, itself within 64 u of the mean
     slack = 64 * 2.0 ** -24 * 64 * 2.0 ** -24 * np.abs(rm[:, None])
     close(y, ry, rr[:, None] * slack + 4e-6 * (1 + np.abs(ry)))
+
+
+@TYPES
+@pytest.mark.parametrize("rows,cols", [(4096, 32), (300, 64), (500, 640), (250, 2048), (60, 4096)])
+def test_layer_norm_rstd_is_rounded_once(rows, cols, dtype):
+    """Rows of a and -a in turn have mean 0 and, for an a of at most 8 bits,
+    variance a^2, sums and quotient exact. eps = 0: rstd is the float32 number
+    nearest to 1 / a, an error of none in what a whole row is scaled by."""
+    a = (128 + np.arange(rows) % 128) * 2.0 ** (np.arange(rows) // 128 % 20 - 15)
+    x = a[:, None] * (1 - 2.0 * (np.arange(cols) % 2))
+    rstd, y = vec(np.zeros(rows)), torch.empty(rows, cols, device="cuda", dtype=dtype)
+    L.lrcnn_layer_norm_forward(matrix(x, dtype), None, None, 0.0, y, rstd=rstd)
+    want = (1 / a).astype(np.float32)
+    got = rstd.cpu().numpy()
+    assert np.array_equal(got, want), f"{(got != want).mean():.2%} of the rows differ"
+    # no variance and no eps, a variance past float32, and one that is NaN
+    x = np.zeros((3, cols))
+    x[1] = 2.0 ** 100 * (1 - 2.0 * (np.arange(cols) % 2))
+    x[2, 5] = math.nan
+    L.lrcnn_layer_norm_forward(matrix(x, dtype), None, None, 0.0, y[:3], rstd=rstd[:3])
+    got = rstd[:3].cpu().numpy()
+    assert got[0] == math.inf and got[1] == 0 and np.isnan(got[2])
