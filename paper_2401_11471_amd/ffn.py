@@ -11,11 +11,15 @@ normalised row (for norm1's backward pass and, with its scale and shift, for W1'
 gradient), of u (and v) and of norm2's normalised row, and two float32
 statistics: cols * 2 + hidden bytes (twice hidden if gated) and a 32nd, where
 bfloat16 copies of what the backward pass reads (x + z, h, u, a and the norms'
-inputs) take four times that or more. a is formed again from u.
+inputs) take four times that or more. a is formed again from u. What a pass
+uses at full width is scratch that blocks share (``scratch=``), so each block
+after the first adds only what it keeps.
 
-Every step runs in the HIP library; the linear products and input gradients
-are 1x1 convolutions. ``python -m paper_2401_11471_amd.ffn`` trains a small
-trunk, block and classifier head on random labelled images.
+The passes and the update of the weights run in the HIP library, the linear
+products and input gradients as 1x1 convolutions; the biases' and norms'
+updates and the weights' transposes are torch operations.
+``python -m paper_2401_11471_amd.ffn`` trains a small trunk, block and classifier
+head on random labelled images.
 """
 from __future__ import annotations
 
@@ -97,11 +101,30 @@ class Norm:
         self.beta.sub_(lr * self.dbeta)
 
 
+class Scratch:
+    """Named byte buffers that blocks use within a pass and keep nothing in: one set
+    for all blocks that run one after the other on one stream."""
+
+    def __init__(self, sizes, device):
+        self.buffers = {k: torch.empty(n, device=device, dtype=torch.uint8)
+                        for k, n in sizes.items()}
+
+    def take(self, name, *shape, dtype=torch.uint8):
+        """The head of a buffer as a tensor."""
+        n = math.prod(shape) * dtype.itemsize
+        if n > self.buffers[name].numel():
+            raise ValueError(f"scratch for {name} has {self.buffers[name].numel()} bytes, "
+                             f"{n} needed: make the largest block first")
+        return self.buffers[name][:n].view(dtype).view(shape)
+
+
 class FeedForward:
-    """The block on [rows][cols] with `hidden` features in the middle."""
+    """The block on [rows][cols] with `hidden` features in the middle. `scratch`: that
+    of another block, at least as large, that runs before or after this one
+    on the same stream; None: its own."""
 
     def __init__(self, rows, cols, hidden, dtype=L.BF16, kind=L.ACT_GELU, gated=False,
-                 device="cuda", seed=0):
+                 device="cuda", seed=0, scratch=None):
         g = torch.Generator().manual_seed(seed)
         self.kind, self.gated, self.hidden = kind, gated, hidden
         wide = 2 * hidden if gated else hidden
@@ -109,16 +132,25 @@ class FeedForward:
         self.lin1 = Linear(rows, cols, wide, dtype, device, g)
         self.lin2 = Linear(rows, hidden, cols, dtype, device, g)
 
-        def full(width):
-            return torch.empty(rows, width, device=device, dtype=torch_dtype(dtype))
-
         def ckpt():
             return torch.empty(L.lrcnn_act8_bytes(rows, hidden), device=device, dtype=torch.uint8)
         # kept from forward to backward: the norms' and these checkpoints
         self.k_u, self.k_v = ckpt(), ckpt() if gated else None
-        # scratch, one set for both passes
-        self.h, self.z, self.u, self.a = full(cols), full(cols), full(wide), full(hidden)
-        self.k_a = ckpt()
+        # scratch of both passes
+        layers = (self.norm1, self.norm2, self.lin1, self.lin2)
+        tdt, n_ws = torch_dtype(dtype), max(layer.ws.numel() for layer in layers)
+        full = {"h": cols, "z": cols, "u": wide, "a": hidden}
+        if scratch is None:
+            sizes = {k: rows * w * tdt.itemsize for k, w in full.items()}
+            sizes.update(k_a=L.lrcnn_act8_bytes(rows, hidden), ws=n_ws)
+            scratch = Scratch(sizes, device)
+        self.scratch = scratch
+        self.h, self.z, self.u, self.a = (scratch.take(k, rows, w, dtype=tdt)
+                                          for k, w in full.items())
+        self.k_a = scratch.take("k_a", L.lrcnn_act8_bytes(rows, hidden))
+        scratch.take("ws", n_ws)
+        for layer in layers:
+            layer.ws = scratch.buffers["ws"]
 
     def saved_bytes(self):
         """Bytes kept from the forward to the backward pass."""

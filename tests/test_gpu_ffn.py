@@ -108,3 +108,33 @@ def test_training(capsys):
     ffn.main()
     losses = [float(l.split()[-1]) for l in capsys.readouterr().out.splitlines() if "loss" in l]
     assert np.isfinite(losses).all() and losses[-1] < 0.5 * losses[0]
+
+
+@pytest.mark.parametrize("gated", [False, True], ids=["gelu", "silu_gated"])
+def test_blocks_in_one_scratch(gated):
+    """Three blocks in a row, the last one narrower, forward and then backward in
+    the scratch of the first: the same bits as with a scratch each."""
+    print(f"blocks in one scratch {gated}", flush=True)
+    rows, cols, kind = 150, 64, L.ACT_SILU if gated else L.ACT_GELU
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x0, d0 = (torch.randn(rows, cols, generator=g, device="cuda").bfloat16() for _ in range(2))
+
+    def run(shared):
+        blocks = []
+        for i, hidden in enumerate((200, 200, 72)):
+            scratch = blocks[0].scratch if shared and blocks else None
+            blocks.append(ffn.FeedForward(rows, cols, hidden, L.BF16, kind, gated, seed=i,
+                                          scratch=scratch))
+        x, d = [x0], [d0]
+        for b in blocks:
+            x.append(torch.empty_like(x0))
+            b.forward(x[-2], x[-1])
+        for b in reversed(blocks):
+            d.append(torch.empty_like(x0))
+            b.backward(d[-2], d[-1])
+        torch.cuda.synchronize()
+        return x + d + [t for b in blocks for t in (b.lin1.dw, b.lin2.dw, b.lin1.db, b.lin2.db,
+                                                    b.norm1.dgamma, b.norm2.dbeta)]
+    own, shared = run(False), run(True)
+    assert all(torch.isfinite(t).all() for t in own)
+    assert all(torch.equal(p, q) for p, q in zip(own, shared))
