@@ -102,6 +102,16 @@ __device__ __forceinline__ TileId panel_tile(const WgArgs &a) {
   return TileId{(int)(8 * p + x), (int)y, (int)z};
 }
 
+// The workgroup's waves wait for each other, their LDS accesses before done. Unlike
+// __syncthreads, which all threads have to reach at one place, this is the hardware's
+// barrier, which counts waves: each may come from code of its own, so long as
+// all come equally often and a whole wave at once.
+__device__ __forceinline__ void waves_meet() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+}
+
 constexpr int least(int a, int b) { return a < b ? a : b; }
 
 // How a thread reads its eight columns of dy.
@@ -383,7 +393,7 @@ __global__ __launch_bounds__(256, W == 256 ? 1 : 2) void wgrad8_kernel(WgArgs a)
       }
       __builtin_amdgcn_sched_barrier(0);
     });
-    __syncthreads();
+    waves_meet();
   };
   auto all_steps = [&](auto d) {
     for (int t = 0; t < steps; t += ST) {
@@ -424,6 +434,11 @@ __global__ __launch_bounds__(256, W == 256 ? 1 : 2) void wgrad8_kernel(WgArgs a)
       if (t == 0 && odd && steps > 1) place(first);
     }
     __syncthreads();
+    // Waves run copies of the loop that differ in the slice summed for db (`wave`
+    // is a scalar: no wave splits). `steps` is the workgroup's, and so is the
+    // number of times that each copy meets the others. (One copy that sums both
+    // slices, one of them times zero, takes 67800 x 2048 x 8192 from 2.07 to 2.26 ms;
+    // one loop that branches at each step spills 2500 registers.)
     const bool want_db = tl.y == 0 || (a.shift && !a.part);
     if (!want_db) all_steps(integral_constant<int, 2>());
     else if (wave < 2) all_steps(integral_constant<int, 0>());
