@@ -138,3 +138,54 @@ def test_blocks_in_one_scratch(gated):
     own, shared = run(False), run(True)
     assert all(torch.isfinite(t).all() for t in own)
     assert all(torch.equal(p, q) for p, q in zip(own, shared))
+
+
+@pytest.mark.parametrize("dtype", [L.F32, L.BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("gated", [False, True], ids=["gelu", "silu_gated"])
+def test_update(gated, dtype):
+    """update(lr) moves every parameter by -lr times its gradient: one rounding to
+    the storage type, 2^-8 or 2^-23 of the value, and float32's product before it.
+    The pass after it gives the bits of a new block with those parameters, so nothing
+    of the old ones is left, the transposed weights among them."""
+    print(f"update {gated} {dtype}", flush=True)
+    rows, cols, hidden, lr, kind = 90, 48, 104, 0.25, L.ACT_SILU if gated else L.ACT_GELU
+    tdt = torch.bfloat16 if dtype == L.BF16 else torch.float32
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x, dy = (torch.randn(rows, cols, generator=g, device="cuda").to(tdt) for _ in range(2))
+
+    def params(b):
+        return [b.lin1.w, b.lin2.w, b.lin1.b, b.lin2.b, b.norm1.gamma, b.norm2.gamma, b.norm1.beta,
+                b.norm2.beta]
+
+    def grads(b):
+        return [b.lin1.dw, b.lin2.dw, b.lin1.db, b.lin2.db, b.norm1.dgamma, b.norm2.dgamma,
+                b.norm1.dbeta, b.norm2.dbeta]
+
+    def step(b):
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        b.forward(x, y)
+        b.backward(dy, dx)
+        torch.cuda.synchronize()
+        return [y, dx] + [t.clone() for t in grads(b)]
+    b = ffn.FeedForward(rows, cols, hidden, dtype, kind, gated, seed=1)
+    first = step(b)
+    old, d = [t.clone() for t in params(b)], first[2:]
+    b.update(lr)
+    for i, (new, was, grad) in enumerate(zip(params(b), old, d)):
+        want = was.double() - lr * grad.double()
+        ulp = 2.0 ** -8 if new.dtype is torch.bfloat16 else 2.0 ** -23
+        assert (new.double() - want).abs().le(ulp * want.abs() + 2.0 ** -23 * was.double().abs()
+                                              + 1e-37).all(), i
+        assert (new != was).float().mean() > 0.5, i
+    for lin in (b.lin1, b.lin2):
+        assert torch.equal(lin.wt, lin.w.t())
+    fresh = ffn.FeedForward(rows, cols, hidden, dtype, kind, gated, seed=2)
+    for t, s in zip(params(fresh), params(b)):
+        t.copy_(s)
+    for lin in (fresh.lin1, fresh.lin2):
+        lin.wt.copy_(lin.w.t())
+    got, want = step(b), step(fresh)
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    # (norm2's dbeta, the sum of dy, is the one result without a parameter in it)
+    assert torch.equal(got[-1], first[-1])
+    assert not any(torch.equal(p, q) for p, q in zip(got[:-1], first))
