@@ -465,7 +465,8 @@ int lrcnn_linear_wgrad_workspace_bytes(int64_t rows, int64_t n_in,
  * x = scale * q + shift per column (float32 [n_in], NULL for 1 and 0):
  *   dw[n][k] = sum over rows of dy[.][n] * x[.][k]   (float32, dense)
  *   db[n]    = sum over rows of dy[.][n]             (float32, nullable)
- * Products are exact, sums float32, for either dtype of dy. A value of dy that
+ * Products are exact, sums float32, for either dtype of dy; but of a float32 dy
+ * what bfloat16 numbers cannot hold, 2^-134 at most, is lost. A value of dy that
  * is not finite makes its row of dw, and its db, not finite (NaN where the
  * exact sum may be an infinity); a group of the checkpoint that stands for NaN
  * makes its 32 columns of dw NaN. ESHAPE beyond 2^24 features, 2^30 rows, a

@@ -39,7 +39,9 @@ struct WgArgs {
   int accumulate;
 };
 
-// hi + mid + lo == v (hi alone where v is not finite)
+// hi + mid + lo == v (hi alone where v is not finite). As bfloat16 the low one is
+// exact above 2^-110, where all its bits are multiples of 2^-133; below, it is
+// rounded to one.
 __device__ __forceinline__ void cut3(float v, float (&p)[3]) {
   p[0] = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
   float r = v - p[0];

@@ -708,3 +708,22 @@ def test_layer_norm_rstd_is_rounded_once(rows, cols, dtype):
     L.lrcnn_layer_norm_forward(matrix(x, dtype), None, None, 0.0, y[:3], rstd=rstd[:3])
     got = rstd[:3].cpu().numpy()
     assert got[0] == math.inf and got[1] == 0 and np.isnan(got[2])
+
+
+@TYPES
+@pytest.mark.parametrize("e", [-105, -118, -126, -131])
+def test_linear_wgrad_of_the_smallest_gradients(e, dtype):
+    """Subnormal numbers count. bfloat16 ones exactly; of a float32 dy the three
+    pieces keep what 2^-133, the smallest bfloat16 number, can hold, so each value is
+    at most 2^-134 off."""
+    n = 64
+    dy = (1 + np.arange(1, n + 1) * 2.0 ** (-23 if dtype == F32 else -2)) * 2.0 ** e
+    t = matrix(np.stack([dy, dy]), dtype)
+    d64 = np64(t)
+    assert (d64 > 0).all()
+    c, q = checkpoint_of(np.full((2, 32), 2.0 ** 40))
+    dw, db = torch.empty(n, 32, device="cuda"), torch.empty(n, device="cuda")
+    L.lrcnn_linear_wgrad(t, c, dw, db=db)
+    off = 2.0 ** -134 if dtype == F32 else 0
+    close(dw, d64.T @ q, off * np.abs(q).sum(0) + 2.0 ** -23 * d64.T @ q)
+    close(db, d64.sum(0), 2 * off + 2.0 ** -23 * d64.sum(0))
