@@ -2,15 +2,18 @@
 // feed-forward block with checkpoints beside their forward pass and in place
 // of their inputs in the backward pass.
 //
-// All four are bound by HBM: two to five streams of 1 to 4 bytes an element,
-// a dozen operations each. A thread takes eight columns (16 bytes of
-// bfloat16), so a quad of lanes holds a group and its maximum takes two
-// quad moves. 1080000 x 512 bf16: pack 315 us, 5.3 TB/s, unpack 312 us; gelu
-// with a checkpoint, 67800 x 8192 bf16, 598 us, 4.7 TB/s; the backward pass of a
-// gated silu from checkpoints, 3136 x 2731 bf16, 18 us, 4.3 TB/s, partly from the
-// Infinity Cache (a device copy of 4 GiB runs at 4.84 TB/s). Eight columns a
-// thread and a thread's rows one after the other: the loads of many waves, not
-// of one, cover the latency. A call of one row takes 3.2 us, a launch's time.
+// Two to five streams of 1 to 4 bytes an element, a dozen operations each: HBM
+// bounds pack, unpack and the silus. A thread takes eight columns (16 bytes of bfloat16), so a
+// quad of lanes holds a group and its maximum takes two quad moves. Calls one
+// after the other in a graph (a device copy of 4 GiB runs at 4.84 TB/s): 1080000 x
+// 512 bf16 pack 300 to 315 us, 5.3 to 5.6 TB/s, unpack 290; gated silu, 67800 x 8192
+// bf16, 563 us, 5.9 TB/s; gelu there 490 us, with a checkpoint 572, 4.6 and 4.9 TB/s,
+// bound by its vector instructions (0.29 a cycle and SIMD counted, where a kernel at
+// the memory's rate has 0.15), from x backward 600 us, 5.5 TB/s; gated silu backward
+// from checkpoints, 3136 x 2731 bf16, 17 to 19 us, 4.0 to 4.6 TB/s, partly from the Infinity
+// Cache. Eight columns a thread and a thread's rows one after the other: the loads
+// of many waves, not of one, cover the latency. A call of one row takes 2.7 us, a
+// launch's time.
 #include "act8.hpp"
 
 #include <type_traits>
@@ -84,9 +87,11 @@ __device__ __forceinline__ float sigmoid(float x) {
 // are then 0 or 1 (so that an infinity takes the function's limit); NaN stays.
 // gelu: u Phi(u), Phi(-|u|) = exp(-u^2/2) R(|u|), R the Mills ratio over
 // sqrt(2 pi), here t P(t) with t = 1 / (1 + 0.3 |u|) and P of degree 7 fitted
-// over [0, 14] to 1.5e-7 of R (4.4e-7 as evaluated in float32); the relative
-// error stays that small in the tail. tanh form: u s(2 k (u + 0.044715 u^3)),
-// k = sqrt(2 / pi).
+// over [0, 14] to 1.5e-7 of R (4.4e-7 as evaluated in float32). The exponential's
+// argument is rounded to float32, which adds some u^2 2^-25 of the value (1.4e-6
+// at -5, 8e-6 at -13); that of the other two likewise. Below -87, where 1 / (1 +
+// exp(-u)) is subnormal, silu is 0. tanh form: u s(2 k (u + 0.044715 u^3)), k =
+// sqrt(2 / pi).
 template <int KIND>
 __device__ __forceinline__ void activate(float u, float &f, float &df) {
   if constexpr (KIND == LRCNN_ACT_RELU) {

@@ -6,10 +6,12 @@
 //             dgamma = sum over rows of dy xh, dbeta = sum over rows of dy
 //
 // Both read a row once: it stays in registers (TPR threads of NV vectors of
-// eight columns) between its statistics and its result. Both are bound by
-// HBM: 67800 x 2048 bf16 with residual and checkpoint 231 us forward (5.4 TB/s),
-// 189 and 5.5 for the join backward from the checkpoint (5.3 TB/s); one row takes
-// 3.4 us, a launch's time. Statistics and sums are float32: the mean first,
+// eight columns) between its statistics and its result. Widths that fill their
+// threads with one vector are bound by HBM: 67800 x 2048 bf16 with residual and
+// checkpoint 229 us forward (5.4 TB/s), 190 and 5.5 for the join backward from the
+// checkpoint (5.2 TB/s). Others are slower, bf16 forward with the checkpoint in TB/s:
+// 1024 columns 4.9, 1100 2.6, 2048 5.1, 2560 3.2, 4096 4.4, 5120 2.9, 8192 3.4; float32
+// 4.7 to 5.4 at all of them. One row takes 3.2 us, a launch's time. Statistics and sums are float32: the mean first,
 // then the centred sum of squares, so a large mean costs no digits of the
 // variance, and for float32 rows the centred sum too, so that it costs none of the
 // normalised values.

@@ -139,13 +139,15 @@ enum Cols {
 // ones: what they give is never stored.
 //
 // 67800 x 2048 x 8192 bf16 (2.27 TFLOP) takes 2.03 to 2.2 ms, 1030 to 1120
-// TFLOP/s: 4.28 million cycles, the matrix pipes busy in 51% of them, at a clock
+// TFLOP/s: 4.3 million cycles, the matrix pipes busy in 50% of them, at a clock
 // that its own power brings down to 1.7 to 2.0 GHz (2.3 in the small calls); this
 // card's library product of the size runs at 1142 with 54% busy. float32
 // 67800 x 2048 x 2048 takes 1.69 ms, three products, 1009 TFLOP/s. Long and
-// narrow calls (540000 x 256 x 173 bf16: 100 us and 8.9 for the join) are near
-// what reading dy and the codes takes (68 us); small float32 ones (392 x 512 x
-// 2048: 19 us) are bound by the instructions that cut dy, on 64 of the CUs.
+// narrow calls (540000 x 256 x 173 bf16: 102 us and 8.9 for the join) take one and
+// a half times what reading dy and the codes takes (68 us): 3.8 TB/s with the matrix
+// pipes 29% busy, a third of that on columns past the 173rd. Small float32 ones
+// (392 x 512 x 2048: 19 us) run 13 steps one after the other on 64 of the CUs, one wave
+// a SIMD with its matrix pipe a quarter and its vector instructions a third of the time.
 template <typename T, int W, int COLS>
 __global__ __launch_bounds__(256, W == 256 ? 1 : 2) void wgrad8_kernel(WgArgs a) {
   constexpr int P = std::is_same<T, float>::value ? 3 : 1;  // pieces of dy
@@ -571,9 +573,11 @@ __global__ __launch_bounds__(256) void wgrad8_join_kernel(WgArgs a, int splits) 
   if (k == 0 && a.db) a.db[n] = a.accumulate ? a.db[n] + d : d;
 }
 
-// Tile width and splits of the rows: the least estimated time, in us, of
+// Tile width and splits of the rows: the least of
 //   steps of a workgroup x time of a step x workgroups of a CU, and, if split,
-//   the join's launch and the partial sums written and read.
+//   the join's launch and the partial sums written and read,
+// in us. The launch, the first loads and the epilogue, 7 to 9 us of a short call, are
+// left out, as every choice has them: it ranks choices and is no call's time.
 // A step of 32 rows takes 0.98 (256-wide bf16 tile, one workgroup a CU), 0.35
 // (128-wide) or 0.82 (128-wide float32); two workgroups a CU share it at 0.85 of
 // twice the time. Measured for splits of the 128-wide tile (us): 1568 x 256 x

@@ -10,8 +10,8 @@ Between forward and backward it keeps, per row, an 8-bit checkpoint of norm1's
 normalised row (for norm1's backward pass and, with its scale and shift, for W1's
 gradient), of u (and v) and of norm2's normalised row, and two float32
 statistics: cols * 2 + hidden bytes (twice hidden if gated) and a 32nd, where
-bfloat16 copies of what the backward pass reads (x + z, h, u, a and the norms'
-inputs) take four times that or more. a is formed again from u. What a pass
+bfloat16 copies of what the backward pass reads (x, h, x + z, u, a and, gated, v)
+take about three times that. a is formed again from u. What a pass
 uses at full width is scratch that blocks share (``scratch=``), so each block
 after the first adds only what it keeps.
 
@@ -208,7 +208,7 @@ def main():
     tr = Trainer(plan, dm, fc, np.zeros(classes), rng.integers(0, classes, batch))
     block = FeedForward(rows, oc, 4 * oc, L.BF16, L.ACT_SILU, gated=True)
     y, dy, dx = (torch.empty(rows, oc, device="cuda", dtype=torch.bfloat16) for _ in range(3))
-    full = 2 * rows * (4 * oc + 3 * 4 * oc)
+    full = 2 * rows * (3 * oc + 3 * 4 * oc)
     print(f"{rows} rows of {oc}: {block.saved_bytes()} bytes kept, {full} in bfloat16")
     for step in range(steps):
         L.lrcnn_forward_rows(plan, dm.x, dm.w, dm.sc, dm.sf, tr.y, tr.ws)
