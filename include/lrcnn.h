@@ -424,8 +424,10 @@ int lrcnn_layer_norm_backward(int64_t rows, int64_t cols, int32_t dtype,
                               int32_t accumulate, void *workspace,
                               size_t ws_bytes, void *stream);
 
-/* Activations: relu; gelu, x * Phi(x); its tanh form; silu, x / (1 + e^-x). */
+/* Activations: relu; gelu, x * Phi(x); its tanh form; silu, x / (1 + e^-x);
+ * none, x itself, where a call says that it takes it. */
 enum {
+  LRCNN_ACT_NONE = -1,
   LRCNN_ACT_RELU = 0,
   LRCNN_ACT_GELU = 1,
   LRCNN_ACT_GELU_TANH = 2,
@@ -477,6 +479,103 @@ int lrcnn_linear_wgrad(int64_t rows, int64_t n_in, int64_t n_out,
                        const float *shift, float *dw, float *db,
                        int32_t accumulate, void *workspace, size_t ws_bytes,
                        void *stream);
+
+/* ---- Group norm of a feature map, dropout and the gated feed-forward block. The
+ * conventions of the entry points above hold. */
+
+/* Device scratch bytes of lrcnn_group_norm_forward and _backward. Never less
+ * than for fewer images or pixels: the workspace of the largest batch or band
+ * serves all of them. */
+int lrcnn_group_norm_workspace_bytes(int64_t batch, int64_t pixels,
+                                     int64_t channels, int64_t groups,
+                                     size_t *bytes);
+
+/* Group norm with an activation, channels last: x is a map of `batch` images of
+ * `pixels` pixels, a matrix of batch * pixels rows and `channels` columns.
+ * Channels go by `groups` equal runs of neighbours; over the pixels and
+ * channels of one group of one image
+ *   xh = (x - mean) * rstd, rstd = 1 / sqrt(var + eps),
+ *   y = f(gamma * xh + beta).
+ * kind: f, an activation or LRCNN_ACT_NONE. gamma, beta: float32 [channels],
+ * NULL for 1 and 0. mean, rstd: float32 [batch][groups], nullable. ckpt
+ * (nullable): receives the checkpoint of xh, for lrcnn_group_norm_backward.
+ * ESHAPE where groups does not divide channels, or beyond 2^20 images or
+ * channels, 2^21 images times groups or 2^23 images times tiles of 512
+ * channels. */
+int lrcnn_group_norm_forward(int64_t batch, int64_t pixels, int64_t channels,
+                             int64_t groups, int32_t dtype, int32_t kind,
+                             const void *x, int64_t ldx, const float *gamma,
+                             const float *beta, float eps, void *y, int64_t ldy,
+                             float *mean, float *rstd, void *ckpt,
+                             void *workspace, size_t ws_bytes, void *stream);
+
+/* Gradients of the group norm with its activation from dy = dL/dy and either
+ * its input x with mean, or ckpt; and rstd:
+ *   e = dy * f'(gamma * xh + beta), q = gamma * e,
+ *   dx = rstd * (q - mean(q) - xh * mean(q * xh)), means over the group,
+ *   dgamma = sum over rows of e * xh, dbeta = sum over rows of e.
+ * dgamma, dbeta: float32 [channels], each nullable. */
+int lrcnn_group_norm_backward(int64_t batch, int64_t pixels, int64_t channels,
+                              int64_t groups, int32_t dtype, int32_t kind,
+                              const void *dy, int64_t lddy, const void *x,
+                              int64_t ldx, const float *mean, const void *ckpt,
+                              const float *rstd, const float *gamma,
+                              const float *beta, void *dx, int64_t lddx,
+                              float *dgamma, float *dbeta, int32_t accumulate,
+                              void *workspace, size_t ws_bytes, void *stream);
+
+/* Dropout whose mask is never stored: y = x * keep / (1 - p) [+ residual],
+ * rounded once; the backward pass is the same call on the gradient, without the
+ * residual. A dropped element counts as 0, whatever x holds there.
+ * rng: two 64-bit numbers in device memory, {seed, offset}, read by the kernel:
+ * a program advances the offset from step to step, also between replays of a
+ * captured graph. site, in [0, 65536): tells the dropouts of one step apart.
+ * first_row: the matrix' first row within a larger one, so that bands and
+ * micro-batches draw what the whole would.
+ * Random bits: Philox4x32-10 (Salmon, Moraes, Dror and Shaw, SC 2011) with the
+ * seed's halves as key and, for g = (first_row + row) * ceil(cols / 8) + col / 8,
+ * the counter (g's low word, g >> 32 | site << 16, the offset's halves). Column c
+ * takes 16 bits of word (c % 8) / 2, the low ones where c is even, and is
+ * dropped where they are less than rint(65536 p); keep / (1 - p) is with that
+ * share. p in [0, 1]. ESHAPE where g could reach 2^48. */
+int lrcnn_dropout(int64_t rows, int64_t cols, int32_t dtype, const void *x,
+                  int64_t ldx, const void *residual, int64_t ldr, double p,
+                  const uint64_t *rng, int32_t site, int64_t first_row, void *y,
+                  int64_t ldy, void *stream);
+
+/* Gated feed-forward block:
+ *   u = x Wu^T + bu, v = x Wv^T + bv, a = f(u) * v, z = a W2^T + b2.
+ * Both projections, the activation and the product are one kernel; z is a second
+ * one on `a` as stored. w1 [2 hidden][n_in] holds Wu, then Wv; w2
+ * [n_out][hidden]; both dense, of the matrices' type. b1 float32 [2 hidden], b2
+ * float32 [n_out], nullable. z may be NULL (w2 and b2 are not read then, n_out is
+ * ignored). For the backward pass, each nullable: uv [rows][2 hidden] receives u
+ * and v; ckpt_u, ckpt_v the checkpoints of their float32 values.
+ * ESHAPE beyond 2^24 features or 2^30 rows. */
+int lrcnn_gated_ffn_forward(int64_t rows, int64_t n_in, int64_t hidden,
+                            int64_t n_out, int32_t dtype, int32_t kind,
+                            const void *x, int64_t ldx, const void *w1,
+                            const float *b1, void *a, int64_t lda, void *uv,
+                            int64_t lduv, void *ckpt_u, void *ckpt_v,
+                            const void *w2, const float *b2, void *z,
+                            int64_t ldz, void *stream);
+
+/* Backward pass of the block from dz = dL/dz:
+ *   da = dz W2, du = da * f'(u) * v, dv = da * f(u), dx = [du dv] W1,
+ * the first three in one kernel, dx from du and dv as stored. u and v come from
+ * uv or from their checkpoints (exactly one of the two). w2t [hidden][n_out] and
+ * w1t [n_in][2 hidden] are the transposed weights, dense. duv [rows][2 hidden]
+ * receives du and dv; ckpt_a (nullable) the checkpoint of f(u) * v; dx (NULL: not
+ * wanted, w1t is not read then, n_in is ignored). The weights' gradients are
+ * lrcnn_linear_wgrad's: of w2 from dz and ckpt_a, of w1 from duv and the
+ * checkpoint of x. ESHAPE beyond 2^24 features or 2^30 rows. */
+int lrcnn_gated_ffn_backward(int64_t rows, int64_t n_in, int64_t hidden,
+                             int64_t n_out, int32_t dtype, int32_t kind,
+                             const void *dz, int64_t lddz, const void *w2t,
+                             const void *uv, int64_t lduv, const void *ckpt_u,
+                             const void *ckpt_v, void *duv, int64_t ldduv,
+                             void *ckpt_a, const void *w1t, void *dx,
+                             int64_t lddx, void *stream);
 
 /* Message of the last failed call on this thread ("" if none). */
 const char *lrcnn_last_error(void);

@@ -25,7 +25,7 @@ F32, BF16 = 0, 1
 CARRY, RECOMPUTE = 0, 1
 EVEN, BALANCED, EXPLICIT, PAPER_2PS = 0, 1, 2, 3
 HYBRID_AUTO = -1
-ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = -1, 0, 1, 2, 3
 
 STATUS = {0: "OK", -1: "EINVAL", -2: "ESHAPE", -3: "EPARTITION",
           -4: "EWORKSPACE", -5: "ESTATE", -6: "EDTYPE", -7: "EHIP",
@@ -79,7 +79,9 @@ _BLOCK_EXPORTS = ("lrcnn_act8_bytes", "lrcnn_act8_pack", "lrcnn_act8_unpack",
                   "lrcnn_layer_norm_forward", "lrcnn_layer_norm_workspace_bytes",
                   "lrcnn_layer_norm_backward", "lrcnn_activation_forward",
                   "lrcnn_activation_backward", "lrcnn_linear_wgrad_workspace_bytes",
-                  "lrcnn_linear_wgrad")
+                  "lrcnn_linear_wgrad", "lrcnn_group_norm_workspace_bytes",
+                  "lrcnn_group_norm_forward", "lrcnn_group_norm_backward", "lrcnn_dropout",
+                  "lrcnn_gated_ffn_forward", "lrcnn_gated_ffn_backward")
 
 
 def _load():
@@ -125,6 +127,17 @@ def _load():
     lib.lrcnn_linear_wgrad_workspace_bytes.argtypes = [i64, i64, i64, i32, psz]
     lib.lrcnn_linear_wgrad.argtypes = [i64, i64, i64, i32, vp, i64, vp, vp, vp, vp, vp, i32, vp,
                                        sz, vp]
+    lib.lrcnn_group_norm_workspace_bytes.argtypes = [i64, i64, i64, i64, psz]
+    lib.lrcnn_group_norm_forward.argtypes = [i64, i64, i64, i64, i32, i32, vp, i64, vp, vp, f32,
+                                             vp, i64, vp, vp, vp, vp, sz, vp]
+    lib.lrcnn_group_norm_backward.argtypes = [i64, i64, i64, i64, i32, i32, vp, i64, vp, i64, vp,
+                                              vp, vp, vp, vp, vp, i64, vp, vp, i32, vp, sz, vp]
+    lib.lrcnn_dropout.argtypes = [i64, i64, i32, vp, i64, vp, i64, C.c_double, vp, i32, i64, vp,
+                                  i64, vp]
+    lib.lrcnn_gated_ffn_forward.argtypes = [i64, i64, i64, i64, i32, i32, vp, i64, vp, vp, vp, i64,
+                                            vp, i64, vp, vp, vp, vp, vp, i64, vp]
+    lib.lrcnn_gated_ffn_backward.argtypes = [i64, i64, i64, i64, i32, i32, vp, i64, vp, vp, i64,
+                                             vp, vp, vp, i64, vp, vp, vp, i64, vp]
     lib.lrcnn_last_error.restype = C.c_char_p
     lib.lrcnn_debug_dry_run.argtypes = [C.c_int]
     lib.lrcnn_debug_dry_run.restype = None
@@ -561,6 +574,137 @@ def lrcnn_linear_wgrad(dy, ckpt, dw, workspace=None, db=None, scale=None, shift=
         _vec("scale", scale, n_in, like), _vec("shift", shift, n_in, like),
         _vec("dw", dw, n_out * n_in, like), _vec("db", db, n_out, like), 1 if accumulate else 0,
         pw, nw, _raw_stream(stream, like)))
+
+
+# ---- group norm of a feature map, dropout, the gated feed-forward block
+def _rows(name, t, cols, like):
+    """Pointer and row stride of a matrix of the first one's rows, dtype and device and
+    `cols` columns (None: absent)."""
+    if t is None:
+        return None, 0
+    if t.shape != (like[0][0], cols) or t.dtype is not like[1] or t.get_device() != like[2]:
+        _einval(f"{name} must be a matrix {(like[0][0], cols)} of {like[1]} on the same device")
+    return t.data_ptr(), _ld(name, t)
+
+
+def _weight(name, t, n_out, n_in, like):
+    """Pointer of a dense weight [n_out][n_in] of the matrices' dtype (None: absent)."""
+    if t is None:
+        return None
+    if t.shape != (n_out, n_in) or t.dtype is not like[1] or t.get_device() != like[2] \
+            or not t.is_contiguous():
+        _einval(f"{name} must be dense [{n_out}][{n_in}] of {like[1]} on the same device")
+    return t.data_ptr()
+
+
+def _images(shape, batch):
+    """Pixels of each of the `batch` images whose rows a matrix holds."""
+    if batch < 0 or (shape[0] % batch if batch else shape[0]):
+        _einval(f"{shape[0]} rows are not {batch} images of as many pixels")
+    return shape[0] // batch if batch else 0
+
+
+def lrcnn_group_norm_workspace_bytes(batch, pixels, channels, groups):
+    return _query(LIB.lrcnn_group_norm_workspace_bytes, batch, pixels, channels, groups)
+
+
+def lrcnn_group_norm_forward(kind, x, gamma, beta, eps, y, batch, groups, workspace, mean=None,
+                             rstd=None, ckpt=None, stream=None):
+    """y = f(group norm of x), f of `kind` (ACT_NONE: x itself); x: [batch * pixels]
+    [channels]; mean, rstd per image and group; ckpt: the checkpoint of the
+    normalised map."""
+    like = _first("x", x)
+    shape, _, _, dt, px, ldx = like
+    cols, pixels = shape[1], _images(shape, batch)
+    py, ldy = _mat("y", y, like)
+    pw, nw = _workspace(workspace, like, lrcnn_group_norm_workspace_bytes, batch, pixels, cols,
+                        groups)
+    _check(LIB.lrcnn_group_norm_forward(
+        batch, pixels, cols, groups, dt, kind, px, ldx, _vec("gamma", gamma, cols, like),
+        _vec("beta", beta, cols, like), eps, py, ldy, _vec("mean", mean, batch * groups, like),
+        _vec("rstd", rstd, batch * groups, like), _ckpt("ckpt", ckpt, shape, like), pw, nw,
+        _raw_stream(stream, like)))
+
+
+def lrcnn_group_norm_backward(kind, dy, rstd, gamma, beta, dx, batch, groups, workspace,
+                              dgamma=None, dbeta=None, x=None, mean=None, ckpt=None,
+                              accumulate=False, stream=None):
+    """dx, dgamma and dbeta from dy and either (x, mean) or ckpt."""
+    like = _first("dy", dy)
+    shape, _, _, dt, pdy, lddy = like
+    cols, pixels = shape[1], _images(shape, batch)
+    px, ldx = _mat("x", x, like)
+    pdx, lddx = _mat("dx", dx, like)
+    pw, nw = _workspace(workspace, like, lrcnn_group_norm_workspace_bytes, batch, pixels, cols,
+                        groups)
+    _check(LIB.lrcnn_group_norm_backward(
+        batch, pixels, cols, groups, dt, kind, pdy, lddy, px, ldx,
+        _vec("mean", mean, batch * groups, like), _ckpt("ckpt", ckpt, shape, like),
+        _vec("rstd", rstd, batch * groups, like), _vec("gamma", gamma, cols, like),
+        _vec("beta", beta, cols, like), pdx, lddx, _vec("dgamma", dgamma, cols, like),
+        _vec("dbeta", dbeta, cols, like), 1 if accumulate else 0, pw, nw,
+        _raw_stream(stream, like)))
+
+
+def lrcnn_dropout(x, y, p, rng, residual=None, site=0, first_row=0, stream=None):
+    """y = x with a share p of its elements dropped, the others over 1 - p
+    (+ residual). rng: int64 [2] on the GPU, the seed and the offset; the same call
+    on the gradient, without residual, is the backward pass."""
+    like = _first("x", x)
+    shape, _, _, dt, px, ldx = like
+    pr, ldr = _mat("residual", residual, like)
+    py, ldy = _mat("y", y, like)
+    if rng.dtype is not torch.int64 or rng.numel() != 2 or not rng.is_contiguous() \
+            or rng.get_device() != like[2]:
+        _einval("rng must be two dense int64 values on the same device")
+    _check(LIB.lrcnn_dropout(shape[0], shape[1], dt, px, ldx, pr, ldr, p, rng.data_ptr(), site,
+                             first_row, py, ldy, _raw_stream(stream, like)))
+
+
+def lrcnn_gated_ffn_forward(kind, x, w1, a, b1=None, w2=None, b2=None, z=None, uv=None,
+                            ckpt_u=None, ckpt_v=None, stream=None):
+    """a = f(x Wu^T + bu) * (x Wv^T + bv), w1 = [Wu; Wv], and with z: z = a w2^T + b2.
+    uv, ckpt_u, ckpt_v: receive what the backward pass reads, full-width or as
+    checkpoints."""
+    like = _first("x", x)
+    (rows, n_in), _, _, dt, px, ldx = like
+    hidden = a.shape[-1]
+    n_out = 0 if z is None else z.shape[-1]
+    pa, lda = _rows("a", a, hidden, like)
+    puv, lduv = _rows("uv", uv, 2 * hidden, like)
+    pz, ldz = _rows("z", z, n_out, like)
+    if (z is None) != (w2 is None) or (b2 is not None and z is None):
+        _einval("z goes with w2 (and b2)")
+    _check(LIB.lrcnn_gated_ffn_forward(
+        rows, n_in, hidden, n_out, dt, kind, px, ldx, _weight("w1", w1, 2 * hidden, n_in, like),
+        _vec("b1", b1, 2 * hidden, like), pa, lda, puv, lduv,
+        _ckpt("ckpt_u", ckpt_u, (rows, hidden), like),
+        _ckpt("ckpt_v", ckpt_v, (rows, hidden), like), _weight("w2", w2, n_out, hidden, like),
+        _vec("b2", b2, n_out, like), pz, ldz, _raw_stream(stream, like)))
+
+
+def lrcnn_gated_ffn_backward(kind, dz, w2t, duv, uv=None, ckpt_u=None, ckpt_v=None, ckpt_a=None,
+                             w1t=None, dx=None, stream=None):
+    """duv = [du dv] from dz, the transposed w2 and either uv or (ckpt_u, ckpt_v);
+    ckpt_a: receives the checkpoint of f(u) * v; with dx: dx = duv W1, w1t the
+    transposed w1."""
+    like = _first("dz", dz)
+    (rows, n_out), _, _, dt, pdz, lddz = like
+    if w2t.dim() != 2:
+        _einval("w2t must be [hidden][n_out]")
+    hidden = w2t.shape[0]
+    n_in = 0 if dx is None else dx.shape[-1]
+    puv, lduv = _rows("uv", uv, 2 * hidden, like)
+    pduv, ldduv = _rows("duv", duv, 2 * hidden, like)
+    pdx, lddx = _rows("dx", dx, n_in, like)
+    if (dx is None) != (w1t is None):
+        _einval("dx goes with w1t")
+    _check(LIB.lrcnn_gated_ffn_backward(
+        rows, n_in, hidden, n_out, dt, kind, pdz, lddz, _weight("w2t", w2t, hidden, n_out, like),
+        puv, lduv, _ckpt("ckpt_u", ckpt_u, (rows, hidden), like),
+        _ckpt("ckpt_v", ckpt_v, (rows, hidden), like), pduv, ldduv,
+        _ckpt("ckpt_a", ckpt_a, (rows, hidden), like),
+        _weight("w1t", w1t, n_in, 2 * hidden, like), pdx, lddx, _raw_stream(stream, like)))
 
 
 def lrcnn_debug_dry_run(on):

@@ -1,0 +1,271 @@
+"""Refusals of the group norm, dropout and gated feed-forward entry points and of
+their binding, and the workspace query: host code only. Nothing is enqueued by a
+refused call."""
+import pytest
+import torch
+
+from paper_2401_11471_amd import lrcnn as L
+
+P = 1 << 20  # a pointer that is never followed
+EINVAL, ESHAPE, EWORKSPACE, EDTYPE = -1, -2, -4, -6
+
+
+def last():
+    return L.LIB.lrcnn_last_error().decode()
+
+
+def gn_fwd(batch=2, pixels=3, cols=8, groups=2, dtype=L.F32, kind=L.ACT_SILU, x=P, ldx=0, gamma=P,
+           beta=P, eps=1e-5, y=P, ldy=0, mean=P, rstd=P, ckpt=None, ws=P, ws_bytes=1 << 40):
+    return L.LIB.lrcnn_group_norm_forward(batch, pixels, cols, groups, dtype, kind, x, ldx, gamma,
+                                          beta, eps, y, ldy, mean, rstd, ckpt, ws, ws_bytes, None)
+
+
+def gn_bwd(batch=2, pixels=3, cols=8, groups=2, dtype=L.F32, kind=L.ACT_SILU, dy=P, x=P, mean=P,
+           ckpt=None, rstd=P, gamma=P, beta=P, dx=P, dgamma=P, dbeta=P, acc=0, ws=P,
+           ws_bytes=1 << 40):
+    return L.LIB.lrcnn_group_norm_backward(batch, pixels, cols, groups, dtype, kind, dy, 0, x, 0,
+                                           mean, ckpt, rstd, gamma, beta, dx, 0, dgamma, dbeta, acc,
+                                           ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("call", [gn_fwd, gn_bwd])
+def test_group_norm_refuses(call):
+    assert call(dtype=2) == EDTYPE
+    for kw in (dict(batch=-1), dict(pixels=-1), dict(cols=0), dict(groups=0), dict(groups=3),
+               dict(groups=-2), dict(batch=(1 << 20) + 1), dict(cols=1 << 21),
+               dict(pixels=1 << 41), dict(batch=1 << 20, pixels=1 << 30),
+               dict(batch=1 << 20, groups=8)):
+        assert call(**kw) == ESHAPE, kw
+    for kind in (-2, 4):
+        assert call(kind=kind) == EINVAL
+    assert call(x=P + 2) == EINVAL and "misaligned" in last()
+    assert call(gamma=P + 1) == EINVAL
+    assert call(beta=P + 2) == EINVAL
+    assert call(mean=P + 2) == EINVAL
+    assert call(rstd=P + 2) == EINVAL
+    assert call(ws=None) == EINVAL
+    assert call(ws=P + 8) == EINVAL
+    need = L.lrcnn_group_norm_workspace_bytes(2, 3, 8, 2)
+    assert call(ws_bytes=need - 1) == EWORKSPACE and str(need) in last()
+
+
+def test_group_norm_forward_refuses():
+    assert gn_fwd(x=None) == EINVAL
+    assert gn_fwd(y=None) == EINVAL
+    assert gn_fwd(ldx=7) == ESHAPE
+    assert gn_fwd(ldy=-8) == ESHAPE
+    assert gn_fwd(ckpt=P + 4) == EINVAL
+    for eps in (-1e-5, float("nan"), float("inf")):
+        assert gn_fwd(eps=eps) == EINVAL
+    # no rows: nothing to do, nothing to check
+    assert gn_fwd(batch=0, x=None, y=None, ws=None) == 0
+    assert gn_fwd(pixels=0, x=None, y=None, ws=None) == 0
+
+
+def test_group_norm_backward_refuses():
+    assert gn_bwd(dy=None) == EINVAL
+    assert gn_bwd(dx=None) == EINVAL
+    assert gn_bwd(rstd=None) == EINVAL
+    assert gn_bwd(x=None, mean=None) == EINVAL       # neither x nor ckpt
+    assert gn_bwd(ckpt=P) == EINVAL                  # both
+    assert gn_bwd(mean=None) == EINVAL               # x without mean
+    assert gn_bwd(x=None, ckpt=P) == EINVAL          # mean without x
+    assert gn_bwd(x=None, mean=None, ckpt=P + 8) == EINVAL
+    assert gn_bwd(dgamma=P + 2) == EINVAL
+    # no rows: gradients that are added to stay as they are
+    assert gn_bwd(batch=0, dy=None, acc=1, ws=None) == 0
+    assert gn_bwd(pixels=0, dy=None, dgamma=None, dbeta=None, ws=None) == 0
+
+
+@pytest.mark.parametrize("cols,groups", [(1, 1), (64, 32), (510, 34), (2048, 32), (5000, 1)])
+def test_group_norm_workspace_serves_fewer(cols, groups):
+    """It never shrinks as images or pixels grow, and stays small beside the map."""
+    sizes = [0, 1, 2, 3, 5, 8, 13, 40, 100, 300, 1000, 4000, 20000, 135000, 540000]
+    need = {(b, p): L.lrcnn_group_norm_workspace_bytes(b, p, cols, groups)
+            for b in sizes[:11] for p in sizes}
+    for b, b2 in zip(sizes[:10], sizes[1:11]):
+        for p, p2 in zip(sizes, sizes[1:]):
+            assert need[b, p] <= need[b2, p] and need[b2, p] <= need[b2, p2]
+    assert need[8, 135000] <= 0.05 * 8 * 135000 * cols * 4 + 4096
+    assert L.LIB.lrcnn_group_norm_workspace_bytes(1, 1, 1, 1, None) == EINVAL
+    with pytest.raises(L.LrcnnError) as e:
+        L.lrcnn_group_norm_workspace_bytes(1, 1, 10, 3)
+    assert e.value.code == ESHAPE
+
+
+def drop(rows=2, cols=8, dtype=L.F32, x=P, ldx=0, res=None, p=0.5, rng=P, site=0, first=0, y=P):
+    return L.LIB.lrcnn_dropout(rows, cols, dtype, x, ldx, res, 0, p, rng, site, first, y, 0, None)
+
+
+def test_dropout_refuses():
+    assert drop(dtype=7) == EDTYPE
+    assert drop(rows=-1) == ESHAPE
+    assert drop(cols=0) == ESHAPE
+    assert drop(x=None) == EINVAL
+    assert drop(y=None) == EINVAL
+    assert drop(x=P + 2) == EINVAL
+    assert drop(res=P + 1) == EINVAL
+    assert drop(ldx=7) == ESHAPE
+    assert drop(rng=None) == EINVAL and "rng" in last()
+    assert drop(rng=P + 4) == EINVAL
+    for p in (-0.1, 1.1, float("nan")):
+        assert drop(p=p) == EINVAL
+    for site in (-1, 65536):
+        assert drop(site=site) == EINVAL
+    for first in (-1, (1 << 48) - 1):
+        assert drop(first=first) == ESHAPE
+    assert drop(rows=0, x=None, rng=None) == 0
+
+
+def ffn_fwd(rows=2, n_in=8, hidden=16, n_out=8, dtype=L.F32, kind=L.ACT_SILU, x=P, ldx=0, w1=P,
+            b1=P, a=P, lda=0, uv=None, lduv=0, ku=None, kv=None, w2=P, b2=P, z=P, ldz=0):
+    return L.LIB.lrcnn_gated_ffn_forward(rows, n_in, hidden, n_out, dtype, kind, x, ldx, w1, b1, a,
+                                         lda, uv, lduv, ku, kv, w2, b2, z, ldz, None)
+
+
+def ffn_bwd(rows=2, n_in=8, hidden=16, n_out=8, dtype=L.F32, kind=L.ACT_SILU, dz=P, lddz=0, w2t=P,
+            uv=P, lduv=0, ku=None, kv=None, duv=P, ldduv=0, ka=None, w1t=P, dx=P, lddx=0):
+    return L.LIB.lrcnn_gated_ffn_backward(rows, n_in, hidden, n_out, dtype, kind, dz, lddz, w2t, uv,
+                                          lduv, ku, kv, duv, ldduv, ka, w1t, dx, lddx, None)
+
+
+@pytest.mark.parametrize("call", [ffn_fwd, ffn_bwd])
+def test_gated_ffn_refuses(call):
+    assert call(dtype=3) == EDTYPE
+    for kw in (dict(rows=-1), dict(n_in=0), dict(hidden=0), dict(n_out=0),
+               dict(hidden=(1 << 23) + 1), dict(n_in=(1 << 24) + 1), dict(n_out=(1 << 24) + 1),
+               dict(rows=(1 << 30) + 1)):
+        assert call(**kw) == ESHAPE, kw
+    for kind in (-1, 4):
+        assert call(kind=kind) == EINVAL
+
+
+def test_gated_ffn_forward_refuses():
+    for k in ("x", "w1", "a", "w2"):
+        assert ffn_fwd(**{k: None}) == EINVAL, k
+        assert ffn_fwd(**{k: P + 2}) == EINVAL, k
+    for k in ("b1", "b2", "z", "uv"):
+        assert ffn_fwd(**{k: P + 2}) == EINVAL, k
+    assert ffn_fwd(ku=P + 4) == EINVAL and ffn_fwd(kv=P + 8) == EINVAL
+    assert ffn_fwd(ldx=7) == ESHAPE and ffn_fwd(lda=15) == ESHAPE and ffn_fwd(ldz=7) == ESHAPE
+    assert ffn_fwd(uv=P, lduv=31) == ESHAPE
+    assert ffn_fwd(rows=0, x=None) == 0
+
+
+def test_gated_ffn_backward_refuses():
+    for k in ("dz", "w2t", "duv", "w1t"):
+        assert ffn_bwd(**{k: None}) == EINVAL, k
+        assert ffn_bwd(**{k: P + 2}) == EINVAL, k
+    assert ffn_bwd(uv=None) == EINVAL                     # neither uv nor checkpoints
+    assert ffn_bwd(ku=P, kv=P) == EINVAL                  # both
+    assert ffn_bwd(uv=None, ku=P) == EINVAL               # one checkpoint
+    assert ffn_bwd(ku=P) == EINVAL
+    assert ffn_bwd(ka=P + 4) == EINVAL
+    assert ffn_bwd(uv=None, ku=P + 4, kv=P) == EINVAL
+    assert ffn_bwd(ldduv=31) == ESHAPE and ffn_bwd(lduv=16) == ESHAPE
+    assert ffn_bwd(lddz=7) == ESHAPE and ffn_bwd(lddx=7) == ESHAPE
+    assert ffn_bwd(rows=0, dz=None) == 0
+
+
+def z(*s, **k):
+    return torch.zeros(*s, **k)
+
+
+def test_binding_refuses_tensors_that_do_not_agree():
+    ws, ck = z(1 << 16, dtype=torch.uint8), z(1 << 14, dtype=torch.uint8)
+    x, c, rng = z(6, 40), z(40), z(2, dtype=torch.int64)
+
+    def refused(code, fn, *a, **k):
+        with pytest.raises(L.LrcnnError) as e:
+            fn(*a, stream=0, **k)
+        assert e.value.code == code, e.value
+    f, S = L.lrcnn_group_norm_forward, L.ACT_SILU
+    refused(EINVAL, f, S, x, c, c, 1e-5, z(6, 41), 2, 4, ws)
+    refused(EINVAL, f, S, x, c, c, 1e-5, x, 4, 4, ws)          # 6 rows are not 4 images
+    refused(EINVAL, f, S, x, c, c, 1e-5, x, 0, 4, ws)
+    refused(EINVAL, f, S, x, z(39), c, 1e-5, x, 2, 4, ws)
+    refused(EINVAL, f, S, x, c, c, 1e-5, x, 2, 4, ws, mean=z(2, 5))
+    refused(EINVAL, f, S, x, c, c, 1e-5, x, 2, 4, ws, ckpt=ck[:100])
+    refused(EINVAL, f, S, x, c, c, 1e-5, x, 2, 4, ws.float())
+    refused(EWORKSPACE, f, S, x, c, c, 1e-5, x, 2, 4, ws[:16])
+    refused(EDTYPE, f, S, x.half(), c, c, 1e-5, x, 2, 4, ws)
+    f = L.lrcnn_group_norm_backward
+    refused(EINVAL, f, S, x, z(2, 4), c, c, x.bfloat16(), 2, 4, ws, x=x, mean=z(2, 4))
+    refused(EINVAL, f, S, x, z(2, 3), c, c, x, 2, 4, ws, x=x, mean=z(2, 4))
+    refused(EINVAL, f, S, x, z(2, 4), c, c, x, 2, 4, ws, x=x, mean=z(2, 4), dgamma=z(4))
+    f = L.lrcnn_dropout
+    refused(EINVAL, f, x, z(6, 39), 0.5, rng)
+    refused(EINVAL, f, x, x, 0.5, rng.int())
+    refused(EINVAL, f, x, x, 0.5, z(3, dtype=torch.int64))
+    refused(EINVAL, f, x, x, 0.5, z(2, 2, dtype=torch.int64)[:, 0])
+    refused(EINVAL, f, x, x, 0.5, rng, residual=x.bfloat16())
+    f, w1, w2 = L.lrcnn_gated_ffn_forward, z(32, 40), z(40, 16)
+    refused(EINVAL, f, S, x, w1, z(6, 17))
+    refused(EINVAL, f, S, x, w1.t(), z(6, 16))
+    refused(EINVAL, f, S, x, z(40, 32).t(), z(6, 16))           # not dense
+    refused(EINVAL, f, S, x, w1.bfloat16(), z(6, 16))
+    refused(EINVAL, f, S, x, w1, z(6, 16), b1=z(16))
+    refused(EINVAL, f, S, x, w1, z(6, 16), uv=z(6, 16))
+    refused(EINVAL, f, S, x, w1, z(6, 16), w2=w2)               # w2 without z
+    refused(EINVAL, f, S, x, w1, z(6, 16), z=z(6, 40))          # z without w2
+    refused(EINVAL, f, S, x, w1, z(6, 16), b2=c)
+    refused(EINVAL, f, S, x, w1, z(6, 16), w2=w2, z=z(6, 39))
+    refused(EINVAL, f, S, x, w1, z(6, 16), ckpt_u=ck[:10])
+    f, w2t, w1t = L.lrcnn_gated_ffn_backward, z(16, 40), z(40, 32)
+    refused(EINVAL, f, S, x, w2t, z(6, 16), uv=z(6, 32))
+    refused(EINVAL, f, S, x, z(16, 39), z(6, 32), uv=z(6, 32))
+    refused(EINVAL, f, S, x, w2t, z(6, 32), uv=z(5, 32))
+    refused(EINVAL, f, S, x, w2t, z(6, 32), uv=z(6, 32), dx=x)
+    refused(EINVAL, f, S, x, w2t, z(6, 32), uv=z(6, 32), w1t=w1t)
+    refused(EINVAL, f, S, x, w2t, z(6, 32), uv=z(6, 32), w1t=w1t, dx=z(6, 41))
+
+
+# name, and a call of host tensors that agree with each other
+CALLS = {
+    "lrcnn_group_norm_forward": lambda b, **k: L.lrcnn_group_norm_forward(
+        L.ACT_SILU, z(6, 40), z(40), z(40), 1e-5, z(6, 40), 2, 4, b, mean=z(2, 4), rstd=z(2, 4),
+        ckpt=b, **k),
+    "lrcnn_group_norm_backward": lambda b, **k: L.lrcnn_group_norm_backward(
+        L.ACT_NONE, z(6, 40), z(2, 4), z(40), z(40), z(6, 40), 2, 4, b, dgamma=z(40), dbeta=z(40),
+        ckpt=b, **k),
+    "lrcnn_dropout": lambda b, **k: L.lrcnn_dropout(
+        z(6, 40), z(6, 40), 0.5, z(2, dtype=torch.int64), residual=z(6, 40), **k),
+    "lrcnn_gated_ffn_forward": lambda b, **k: L.lrcnn_gated_ffn_forward(
+        L.ACT_GELU, z(6, 40), z(32, 40), z(6, 16), b1=z(32), w2=z(8, 16), b2=z(8), z=z(6, 8),
+        ckpt_u=b, ckpt_v=b, **k),
+    "lrcnn_gated_ffn_backward": lambda b, **k: L.lrcnn_gated_ffn_backward(
+        L.ACT_GELU, z(6, 8), z(16, 8), z(6, 32), ckpt_u=b, ckpt_v=b, ckpt_a=b, w1t=z(40, 32),
+        dx=z(6, 40), **k),
+}
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+@pytest.mark.parametrize("stream", [{}, {"stream": 0}], ids=["current", "given"])
+def test_binding_refuses_host_tensors(name, stream, monkeypatch):
+    """Host memory never reaches the library, whose kernels would follow its pointers."""
+    reached = []
+    monkeypatch.setattr(L.LIB, name, lambda *a: reached.append(a) or 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 0, raising=False)
+    with pytest.raises(L.LrcnnError) as e:
+        CALLS[name](z(1 << 16, dtype=torch.uint8), **stream)
+    assert e.value.code == EINVAL and "GPU" in str(e.value)
+    assert not reached
+
+
+@pytest.mark.parametrize("stream", [None, 0, 77])
+def test_binding_refuses_tensors_of_another_gpu(stream, monkeypatch):
+    """Tensors of GPU 1 are worked on while it is current, in its stream, and refused
+    while GPU 0 is: the library launches on the current device."""
+    calls = []
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 100 + dev, raising=False)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 1)
+    for name, call in CALLS.items():
+        monkeypatch.setattr(L.LIB, name, lambda *a: calls.append(a[-1]) or 0)
+        run = lambda: call(z(1 << 16, dtype=torch.uint8), stream=stream)
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+        with pytest.raises(L.LrcnnError) as e:
+            run()
+        assert e.value.code == EINVAL and "cuda:1" in str(e.value) and not calls
+        monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
+        run()
+        assert calls.pop() == (101 if stream is None else stream) and not calls

@@ -1,0 +1,433 @@
+"""Group norm with an activation and dropout on the GPU against the float64 oracle:
+one pixel and one channel on, groups of any width, ragged widths, slices with odd
+strides, no rows, large means, values that are not finite, checkpoints, graphs and
+streams.
+
+Tolerances, with u = 2^-24 (float32 rounding). A group's mean is off by a rounding for
+each join on the longest path (eight pixels, a thread's batches, six halvings;
+slabs and channels in 64 bits), less than 32 of them at these sizes: 32 u of the
+largest magnitude; its variance, of centred values, by 40 u of itself, so rstd by 20 u.
+gamma xh + beta adds four roundings. The activations are evaluated to 4e-6 of their
+argument, slopes below 1.2. A sum over rows takes at most 160 additions in a row.
+A bfloat16 result adds half an ulp, 2^-9 of the value, taken as 2^-8 where the
+value itself is uncertain by the float32 error. Random bits are exact."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import block as OB
+from oracle import map_ops as OM
+from paper_2401_11471_amd import lrcnn as L
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+F32, BF16 = torch.float32, torch.bfloat16
+TYPES = pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+KINDS = {"none": L.ACT_NONE, "relu": L.ACT_RELU, "gelu": L.ACT_GELU, "gelu_tanh": L.ACT_GELU_TANH,
+         "silu": L.ACT_SILU}
+# batch, pixels, channels, groups
+SHAPES = [(1, 1, 1, 1), (1, 1, 8, 8), (3, 1, 12, 4), (2, 2, 7, 7), (2, 5, 30, 2), (1, 49, 512, 32),
+          (7, 169, 510, 34), (2, 300, 96, 8), (5, 33, 33, 1), (1, 1000, 20, 20), (3, 130, 2048, 32),
+          (2, 777, 1100, 11), (130, 9, 40, 5), (1, 3000, 64, 1), (9, 64, 64, 16), (2, 17, 5000, 4)]
+SIZES = pytest.mark.parametrize("batch,pixels,cols,groups", SHAPES)
+
+
+def tell(*a):
+    print(*a, flush=True)
+
+
+def matrix(a, dtype, pad=0, at=0):
+    """a on the GPU; pad > 0: a slice of a wider matrix from column `at`, NaN
+    around it."""
+    t = torch.from_numpy(np.asarray(a, np.float32)).to("cuda", dtype)
+    if not pad:
+        return t.contiguous()
+    rows, cols = t.shape
+    wide = torch.full((rows, cols + pad), float("nan"), device="cuda", dtype=dtype)
+    s = wide[:, at:at + cols]
+    s.copy_(t)
+    return s
+
+
+def untouched(s, at):
+    """Nothing beside the slice was written."""
+    cols = s.shape[1]
+    assert torch.isnan(s._base[:, :at]).all() and torch.isnan(s._base[:, at + cols:]).all()
+
+
+def vec(a):
+    return torch.from_numpy(np.asarray(a, np.float32)).cuda()
+
+
+def np64(t):
+    return t.double().cpu().numpy()
+
+
+def buf(n):
+    return torch.full((max(int(n), 16),), 0xA5, device="cuda", dtype=torch.uint8)
+
+
+def checkpoint_of(x):
+    """A checkpoint on the GPU, made by the oracle, and what it stands for."""
+    q, e = OB.encode(x)
+    return torch.from_numpy(OB.pack_bytes(q, e)).cuda(), OB.decode(q, e, x.shape[1])
+
+
+def workspace(batch, pixels, cols, groups):
+    return buf(L.lrcnn_group_norm_workspace_bytes(batch, pixels, cols, groups))
+
+
+def close(got, ref, tol, dtype=F32):
+    got = np64(got).reshape(ref.shape)
+    assert np.isfinite(got).all()
+    over = np.abs(got - ref) - (tol + np.abs(ref) * (2.0 ** -8 if dtype == BF16 else 0) + 1e-37)
+    assert (over <= 0).all(), f"off by {np.abs(got - ref).max():.3g}, {over.max():.3g} over"
+
+
+def features(rng, rows, cols):
+    x = rng.standard_normal((rows, cols)) * np.exp(0.5 * rng.standard_normal(cols))
+    x += 0.5 * rng.standard_normal(cols)
+    x[3::7] = 0
+    return x
+
+
+def t_error(x, xh, t, rstd, batch, groups, gamma, beta):
+    """Bound on the error of gamma xh + beta."""
+    pixels, cols = x.shape[0] // batch, x.shape[1]
+    top = np.abs(x).reshape(batch, pixels, groups, -1).max((1, 3))
+    off = OM.spread(rstd * top, pixels, cols) * 32 * U
+    return np.abs(gamma) * (off + 24 * U * np.abs(xh)) + 4 * U * (np.abs(gamma * xh) + np.abs(beta))
+
+
+def held_close(ckpt, ref, err):
+    """A checkpoint's values against the full ones, known to err: half a step."""
+    q, e = OB.unpack_bytes(ckpt.cpu().numpy(), *ref.shape)
+    step = np.repeat(np.exp2(e.astype(np.float64) - 133), 32, 1)[:, :ref.shape[1]]
+    assert (np.abs(OB.decode(q, e, ref.shape[1]) - ref) <= 0.5 * step + err).all()
+    # the step fits the group's largest value
+    assert (np.abs(e.astype(int) - OB.encode(ref)[1]) <= 1).all()
+    pad = q[:, ref.shape[1]:]
+    assert (pad == 0).all()
+
+
+# -------------------------------------------------------------- group norm
+@TYPES
+@SIZES
+def test_group_norm_forward(batch, pixels, cols, groups, dtype):
+    rng = np.random.default_rng(pixels + cols)
+    rows, ws = batch * pixels, workspace(batch, pixels, cols, groups)
+    gamma, beta = vec(1 + 0.3 * rng.standard_normal(cols)), vec(0.3 * rng.standard_normal(cols))
+    for i, (kind, k) in enumerate(KINDS.items()):
+        pad, at = [(0, 0), (3, 1), (8, 8), (5, 2), (16, 0)][i]
+        tell("group norm", batch, pixels, cols, groups, dtype, kind, pad)
+        x = matrix(features(rng, rows, cols), dtype, pad, at)
+        y = matrix(np.zeros((rows, cols)), dtype, pad, at)
+        mean, rstd = (torch.full((batch, groups), math.nan, device="cuda") for _ in range(2))
+        ck = buf(L.lrcnn_act8_bytes(rows, cols)) if i % 2 else None
+        L.lrcnn_group_norm_forward(k, x, gamma, beta, 1e-3, y, batch, groups, ws, mean=mean,
+                                   rstd=rstd, ckpt=ck)
+        X, ga, be = np64(x), np64(gamma), np64(beta)
+        ry, t, xh, rm, rr = OM.group_norm(X, batch, groups, ga, be, np.float64(np.float32(1e-3)), kind)
+        top = np.abs(X).reshape(batch, pixels, groups, -1).max((1, 3))
+        close(mean, rm, 32 * U * top)
+        close(rstd, rr, 22 * U * rr)
+        err = t_error(X, xh, t, rr, batch, groups, ga, be)
+        close(y, ry, 1.2 * err + (4e-6 * np.abs(t) if kind != "none" else 0), dtype)
+        if ck is not None:
+            one, zero = np.ones(cols), np.zeros(cols)
+            held_close(ck, xh, t_error(X, xh, xh, rr, batch, groups, one, zero))
+        if pad:
+            untouched(y, at)
+    # in place, without gamma, beta and statistics: the same as with ones and zeros
+    L.lrcnn_group_norm_forward(k, x, torch.ones_like(gamma), torch.zeros_like(beta), 1e-3, y, batch,
+                               groups, ws)
+    L.lrcnn_group_norm_forward(k, x, None, None, 1e-3, x, batch, groups, ws)
+    assert torch.equal(x, y)
+
+
+def test_group_norm_of_constant_large_and_bad_images():
+    batch, pixels, cols, groups = 6, 700, 24, 3
+    rng = np.random.default_rng(0)
+    a = rng.standard_normal((batch, pixels, cols))
+    a[0] = 12345.678           # constant: beta exactly
+    a[1] += 4096               # a mean far from zero
+    a[1, :64] = 0              # behind a stripe of padding
+    a[2, 650, 5] = math.nan    # its group alone
+    a[3, 3, 23] = math.inf
+    a[4] *= 1e-20
+    x = matrix(a.reshape(-1, cols), F32)
+    y, ws = torch.empty_like(x), workspace(batch, pixels, cols, groups)
+    mean, rstd = (torch.empty(batch, groups, device="cuda") for _ in range(2))
+    ck = buf(L.lrcnn_act8_bytes(batch * pixels, cols))
+    beta = vec(rng.standard_normal(cols))
+    L.lrcnn_group_norm_forward(L.ACT_NONE, x, None, beta, 1e-5, y, batch, groups, ws, mean, rstd, ck)
+    Y, X = y.view(batch, pixels, cols), np64(x)
+    assert torch.equal(Y[0], beta.expand(pixels, cols))
+    ry, _, xh, rm, rr = OM.group_norm(X, batch, groups, 1.0, np64(beta),
+                                      np.float64(np.float32(1e-5)), "none")
+    ok = np.isfinite(xh).reshape(batch, pixels, cols)
+    got = np64(Y)
+    assert np.isnan(got[2, :, :8]).all() and np.isfinite(got[2, :, 8:]).all()
+    assert np.isnan(got[3, :, 16:]).all() and np.isfinite(got[3, :, :16]).all()
+    assert np.isfinite(got[[0, 1, 4, 5]]).all()
+    ref = ry.reshape(got.shape)
+    top = np.nan_to_num(np.abs(X).reshape(batch, pixels, groups, -1).max((1, 3)), posinf=0)
+    err = OM.spread(np.nan_to_num(rr) * top * 32 * U, pixels, cols).reshape(got.shape)
+    tol = err + 24 * U * np.abs(ref) + 1e-6
+    assert (np.abs(got - ref) <= tol)[ok].all()
+    assert np.abs(np64(rstd)[1] / rr[1] - 1).max() < 40 * U
+    q, e = OB.unpack_bytes(ck.cpu().numpy(), batch * pixels, cols)
+    e = e.reshape(batch, pixels)
+    assert (e[2] == 255).all() and (e[3] == 255).all() and (e[[0, 1, 4, 5]] < 255).all()
+
+
+@TYPES
+@SIZES
+def test_group_norm_backward(batch, pixels, cols, groups, dtype):
+    rng = np.random.default_rng(pixels * 3 + cols)
+    rows, ws = batch * pixels, workspace(batch, pixels, cols, groups)
+    gamma, beta = vec(1 + 0.3 * rng.standard_normal(cols)), vec(0.3 * rng.standard_normal(cols))
+    ga, be = np64(gamma), np64(beta)
+    for i, (kind, k) in enumerate(KINDS.items()):
+        for saved in (False, True):
+            pad, at = [(0, 0), (3, 1), (8, 8), (5, 2), (16, 0)][i]
+            tell("group norm backward", batch, pixels, cols, groups, dtype, kind, saved)
+            x = matrix(features(rng, rows, cols), dtype, pad, at)
+            dy = matrix(rng.standard_normal((rows, cols)), dtype, pad, at)
+            dx = matrix(np.zeros((rows, cols)), dtype, pad, at)
+            _, _, xh, mean, rstd = OM.group_norm(np64(x), batch, groups, ga, be, 1e-3, kind)
+            mean, rstd = vec(mean), vec(rstd)
+            m, r = np64(mean), np64(rstd)
+            kw = dict(x=x, mean=mean)
+            xh = (np64(x) - OM.spread(m, pixels, cols)) * OM.spread(r, pixels, cols)
+            if saved:
+                ck, xh = checkpoint_of(xh)
+                kw = dict(ckpt=ck)
+            dg, db = torch.full((2, cols), 0.5, device="cuda").unbind(0)
+            acc = i % 2
+            L.lrcnn_group_norm_backward(k, dy, rstd, gamma, beta, dx, batch, groups, ws, dgamma=dg,
+                                        dbeta=db, accumulate=acc, **kw)
+            d, t = np64(dy), xh * ga + be
+            rx, rg, rb = OM.group_norm_backward(d, xh, r, batch, groups, ga, be, kind)
+            # xh: two roundings; the slope: as the value, and at relu's kink either side
+            et = np.abs(ga * xh) * 3 * U + 2 * U * np.abs(t)
+            te = np.abs(d) * (1.2 * et + (4e-6 * (1 + np.abs(t)) if kind != "none" else 0) + 2 * U)
+            if kind == "relu":
+                te += np.abs(d) * (np.abs(t) <= 2 * et)
+            e = d * OM._act(t, kind)[1]
+            q = e * ga
+            tq = np.abs(ga) * te + 2 * U * np.abs(q)
+            per = lambda v: OM.spread(v.reshape(batch, pixels, groups, -1).mean((1, 3)), pixels, cols)
+            m1, m2 = per(q), per(q * xh)
+            e1 = per(tq) + 160 * U * per(np.abs(q))
+            e2 = per(tq * np.abs(xh)) + 163 * U * per(np.abs(q * xh))
+            tx = OM.spread(r, pixels, cols) * (
+                tq + e1 + np.abs(xh) * e2
+                + 4 * U * (np.abs(q) + np.abs(m1) + 2 * np.abs(xh * m2)))
+            close(dx, rx, tx, dtype)
+            close(dg, rg + 0.5 * acc, (te * np.abs(xh)).sum(0) + 163 * U * np.abs(e * xh).sum(0) + U)
+            close(db, rb + 0.5 * acc, te.sum(0) + 160 * U * np.abs(e).sum(0) + U)
+            if pad:
+                untouched(dx, at)
+    # in place, one gradient alone: the same
+    L.lrcnn_group_norm_backward(k, dy, rstd, gamma, beta, dy, batch, groups, ws, dbeta=dg, **kw)
+    assert torch.equal(dx, dy)
+
+
+def test_group_norm_backward_by_differences():
+    """dx and the parameters' gradients against differences of the forward kernel in
+    float32: 2 eps = 2^-5 apart, whose own error is some 1e-3."""
+    batch, pixels, cols, groups = 2, 6, 12, 3
+    rng = np.random.default_rng(1)
+    x, dy = (vec(rng.standard_normal((batch * pixels, cols))) for _ in range(2))
+    gamma, beta = vec(1 + 0.2 * rng.standard_normal(cols)), vec(0.2 * rng.standard_normal(cols))
+    ws, y, eps = workspace(batch, pixels, cols, groups), torch.empty_like(x), 2.0 ** -6
+    mean, rstd = (torch.empty(batch, groups, device="cuda") for _ in range(2))
+
+    def f():
+        L.lrcnn_group_norm_forward(L.ACT_SILU, x, gamma, beta, 1e-3, y, batch, groups, ws, mean, rstd)
+        return float((y.double() * dy.double()).sum())
+    f()
+    dx, dg, db = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(beta)
+    L.lrcnn_group_norm_backward(L.ACT_SILU, dy, rstd, gamma, beta, dx, batch, groups, ws, dgamma=dg,
+                                dbeta=db, x=x, mean=mean)
+    for v, g in ((x, dx), (gamma, dg), (beta, db)):
+        flat, grad = v.view(-1), g.view(-1)
+        for i in range(0, flat.numel(), 5):
+            old = flat[i].clone()
+            flat[i] = old + eps
+            hi = f()
+            flat[i] = old - eps
+            lo = f()
+            flat[i] = old
+            assert abs((hi - lo) / (2 * eps) - float(grad[i])) < 5e-3
+
+
+def test_group_norm_without_rows():
+    x, c = torch.empty(0, 16, device="cuda"), torch.ones(16, device="cuda")
+    for batch in (0, 3):
+        ws, s = workspace(batch, 0, 16, 2), torch.empty(batch, 2, device="cuda")
+        L.lrcnn_group_norm_forward(L.ACT_SILU, x, c, c, 1e-5, x, batch, 2, ws, mean=s, rstd=s)
+        for acc, want in ((True, 7.0), (False, 0.0)):
+            dg, db = torch.full((2, 16), 7.0, device="cuda").unbind(0)
+            L.lrcnn_group_norm_backward(L.ACT_SILU, x, s, c, c, x, batch, 2, ws, dgamma=dg, dbeta=db,
+                                        x=x, mean=s, accumulate=acc)
+            assert (dg == want).all() and (db == want).all()
+
+
+def test_group_norm_past_32_bits():
+    """Rows more than 2^32 bytes from the first, in the last of three images."""
+    batch, pixels, cols, groups, ld = 3, 700, 40, 5, 1 << 20
+    tell("group norm past 32 bits")
+    wide = torch.empty(batch * pixels, ld, device="cuda", dtype=BF16)
+    x = wide[:, 8:8 + cols]
+    x.copy_(torch.randn(batch * pixels, cols, device="cuda"))
+    out = [torch.empty(batch * pixels, cols, device="cuda", dtype=BF16) for _ in range(2)]
+    ws = workspace(batch, pixels, cols, groups)
+    L.lrcnn_group_norm_forward(L.ACT_GELU, x, None, None, 1e-5, out[0], batch, groups, ws)
+    L.lrcnn_group_norm_forward(L.ACT_GELU, x.contiguous(), None, None, 1e-5, out[1], batch, groups, ws)
+    assert torch.equal(*out)
+    y = wide[:, 64:64 + cols]
+    L.lrcnn_group_norm_forward(L.ACT_GELU, x, None, None, 1e-5, y, batch, groups, ws)
+    assert torch.equal(y, out[0])
+
+
+@TYPES
+def test_group_norm_in_bands(dtype):
+    """The workspace of the largest call serves smaller ones, whatever it holds."""
+    rng = np.random.default_rng(2)
+    cols, groups = 64, 8
+    ws = workspace(9, 400, cols, groups)
+    for batch, pixels in [(9, 400), (9, 7), (1, 400), (4, 133)]:
+        x = matrix(features(rng, batch * pixels, cols), dtype)
+        y, ref = torch.empty_like(x), torch.empty_like(x)
+        L.lrcnn_group_norm_forward(L.ACT_SILU, x, None, None, 1e-5, y, batch, groups, ws)
+        L.lrcnn_group_norm_forward(L.ACT_SILU, x, None, None, 1e-5, ref, batch, groups,
+                                   workspace(batch, pixels, cols, groups))
+        assert torch.equal(y, ref)
+
+
+# ------------------------------------------------------------------ dropout
+@TYPES
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 7), (3, 8), (2, 9), (65, 33), (300, 64),
+                                       (7, 2048), (130, 2731), (5000, 3)])
+def test_dropout(rows, cols, dtype):
+    rng = np.random.default_rng(rows + cols)
+    for i, p in enumerate([0.0, 0.1, 0.5, 0.9, 1.0]):
+        pad, at = [(0, 0), (3, 1), (8, 8), (5, 2), (16, 0)][i]
+        seed, offset = (int(v) for v in rng.integers(-2 ** 63, 2 ** 63 - 1, 2))
+        site, first = int(rng.integers(0, 65536)), int(rng.integers(0, 2 ** 33))
+        tell("dropout", rows, cols, dtype, p, seed, offset, site, first)
+        state = torch.tensor([seed, offset], device="cuda")
+        x = matrix(rng.standard_normal((rows, cols)) + 3, dtype, pad, at)
+        res = matrix(rng.standard_normal((rows, cols)), dtype, pad, at)
+        y, z = (matrix(np.zeros((rows, cols)), dtype, pad, at) for _ in range(2))
+        kw = dict(site=site, first_row=first)
+        L.lrcnn_dropout(x, y, p, state, **kw)
+        L.lrcnn_dropout(x, z, p, state, residual=res, **kw)
+        bits = OM.dropout_bits(seed, offset, rows, cols, **kw)
+        X, R = np64(x), np64(res)
+        ref = OM.dropout(X, p, bits)
+        assert np.array_equal(np64(y) == 0, ref == 0)
+        close(y, ref, 3 * U * np.abs(ref), dtype)
+        ref = OM.dropout(X, p, bits, R)
+        # (dropped where the bits are less than the rounded 65536 p, so that is what the
+        # bound follows: at 0.9, 58982.4 rounds to 58982, and bits of 58982 are kept)
+        gone = bits < round(65536 * p)
+        close(z, ref, 4 * U * (np.abs(X) / max(1 - p, 1e-5) * ~gone + np.abs(R)), dtype)
+        assert np.array_equal(np64(z)[gone], R[gone])
+        if pad:
+            untouched(y, at)
+        # a band draws what the whole draws
+        if rows > 2:
+            part = matrix(np.zeros((rows - 2, cols)), dtype)
+            L.lrcnn_dropout(x[2:], part, p, state, site=site, first_row=first + 2)
+            assert torch.equal(part, y[2:])
+        # in place
+        L.lrcnn_dropout(x, x, p, state, **kw)
+        assert torch.equal(x, y)
+
+
+def test_dropout_of_bad_values():
+    """What is dropped counts as zero, whatever it holds."""
+    state = torch.tensor([3, 4], device="cuda")
+    for bad in (math.nan, math.inf, -math.inf):
+        x = torch.full((40, 50), bad, device="cuda")
+        y = torch.empty_like(x)
+        L.lrcnn_dropout(x, y, 0.5, state)
+        gone = torch.from_numpy(OM.dropout_bits(3, 4, 40, 50) < 32768).cuda()
+        assert (y[gone] == 0).all() and not torch.isfinite(y[~gone]).any()
+
+
+def test_dropout_is_its_own_backward():
+    """The gradient of the sum of dy y is the same call on dy: x . call(dy) =
+    call(x) . dy, in float64 on float32 results, 4 u of the terms' magnitudes."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x, dy = (torch.randn(200, 77, generator=g, device="cuda") for _ in range(2))
+    state, y, dx = torch.tensor([9, 1], device="cuda"), torch.empty_like(x), torch.empty_like(x)
+    L.lrcnn_dropout(x, y, 0.3, state, site=5)
+    L.lrcnn_dropout(dy, dx, 0.3, state, site=5)
+    a, b = y.double() * dy.double(), dx.double() * x.double()
+    assert (a - b).abs().le(4 * U * a.abs()).all()
+
+
+def test_dropout_past_32_bits():
+    rows, cols = (1 << 22) + 5, 1040
+    tell("dropout past 32 bits", rows, cols)
+    x = torch.ones(rows, cols, device="cuda", dtype=BF16)
+    y, state = torch.empty_like(x), torch.tensor([1, 2], device="cuda")
+    L.lrcnn_dropout(x, y, 0.5, state, first_row=1 << 30)
+    keep = OM.dropout_bits(1, 2, 5, cols, first_row=(1 << 30) + rows - 5) >= 32768
+    assert np.array_equal(np64(y[-5:]), 2.0 * keep)
+    assert abs(float((y == 0).float().mean()) - 0.5) < 1e-3
+
+
+# ---------------------------------------------------------- graphs, streams
+def test_in_a_graph_and_on_a_stream():
+    """A captured step of norm, dropout and both gradients: every replay, with the offset
+    advanced in device memory and eager work between, equals the eager result."""
+    batch, pixels, cols, groups, p = 3, 200, 48, 6, 0.25
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, dy = (torch.randn(batch * pixels, cols, generator=g, device="cuda") for _ in range(2))
+    c = torch.randn(cols, generator=g, device="cuda")
+    state = torch.tensor([11, 0], device="cuda")
+
+    def buffers():
+        s = {k: torch.empty_like(x) for k in ("y", "z", "dz", "dx")}
+        s.update({k: torch.empty(batch, groups, device="cuda") for k in ("mean", "rstd")})
+        s.update({k: torch.empty(cols, device="cuda") for k in ("dg", "db")})
+        s["ws"] = workspace(batch, pixels, cols, groups)
+        return s
+
+    def step(s):
+        L.lrcnn_group_norm_forward(L.ACT_SILU, x, c, c, 1e-5, s["y"], batch, groups, s["ws"],
+                                   s["mean"], s["rstd"])
+        L.lrcnn_dropout(s["y"], s["z"], p, state, residual=x)
+        L.lrcnn_dropout(dy, s["dz"], p, state)
+        L.lrcnn_group_norm_backward(L.ACT_SILU, s["dz"], s["rstd"], c, c, s["dx"], batch, groups,
+                                    s["ws"], dgamma=s["dg"], dbeta=s["db"], x=x, mean=s["mean"])
+    s, e = buffers(), buffers()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(s)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(s)
+    seen = []
+    for i in range(4):
+        state[1] = i
+        x.mul_(1.25)
+        for k in ("y", "z", "dx", "dg", "db"):
+            s[k].fill_(math.nan)
+        graph.replay()
+        step(e)
+        torch.cuda.synchronize()
+        for k in ("y", "z", "dz", "dx", "dg", "db", "mean", "rstd"):
+            assert torch.equal(s[k], e[k]), (i, k)
+        seen.append(s["dz"] == 0)
+    assert all((seen[0] != m).float().mean() > 0.2 for m in seen[1:])
