@@ -42,165 +42,60 @@ struct FfnArgs {
   Ckpt ku, kv, ka;
 };
 
-// ------------------------------------------------------- wave halves
-// A 32 x 32 block of the result: register 4 g + e of a lane is feature
-// 8 g + 4 (lane >> 5) + e of row lane & 31 -- of the eight quads of features the
-// lower half of the wave has the even ones. Exchanged: the lower half has the
-// first 16 features of the row in order, the upper half the last 16.
-__device__ __forceinline__ void swap_halves(uint32_t &x, uint32_t &y) {
-  const auto r = __builtin_amdgcn_permlane32_swap(x, y, false, false);
-  x = r[0], y = r[1];
+// ------------------------------------------------------------- results
+// f(0), f(1), ... f(N - 1), the index a constant
+template <int B, int E, typename F>
+__device__ __forceinline__ void each(F &&f) {
+  if constexpr (B < E) {
+    f(std::integral_constant<int, B>());
+    each<B + 1, E>(f);
+  }
 }
-// N registers a quad, natural quads <-> 16 in a row (the exchange is its own inverse)
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+// The wave's LDS accesses before are done as its other lanes see them
+__device__ __forceinline__ void wave_meets() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+// Results leave the accumulators by strips of 32 rows through a wave's own LDS, float32
+// [32][32 FB]: registers 4 g .. 4 g + 3 of a 32 x 32 block are features 8 g + 4 (lane / 32)
+// on of row lane % 32. They are read back eight features to a lane, a row's
+// lanes next to each other: whole cache lines to memory, a checkpoint's group in a quad of
+// lanes, and one copy of the code for all strips (unrolled over the accumulators it
+// is fetched anew for every tile and takes three times as long). 16-byte slots are
+// swapped by the row, so the lanes of a pass take different banks.
+template <int FB>
+__device__ __forceinline__ lds_char *slot_of(lds_char *l, int row, int slot) {
+  return l + (row * 8 * FB + (slot ^ (row & 7))) * 16;
+}
+template <int FB>
+__device__ __forceinline__ void strip_put(lds_char *l, int i, const f32x16 &b) {
+  const int row = threadIdx.x & 31, half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+  for (int g = 0; g < 4; ++g)
+    *(lds_f32x4 *)slot_of<FB>(l, row, 8 * i + 2 * g + half) =
+        (f32x4){b[4 * g], b[4 * g + 1], b[4 * g + 2], b[4 * g + 3]};
+}
+template <int FB>
+__device__ __forceinline__ void strip_get(lds_char *l, int row, int slot, float (&v)[8]) {
+  const f32x4 x = *(lds_f32x4 *)slot_of<FB>(l, row, slot);
+  const f32x4 y = *(lds_f32x4 *)slot_of<FB>(l, row, slot + 1);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = x[i], v[4 + i] = y[i];
+}
+__device__ __forceinline__ uint2 lds_pair(const lds_char *p) {
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 v = *(__attribute__((address_space(3))) const u32x2 *)p;
+  return make_uint2(v.x, v.y);
+}
+// f of the call's kind (the same branch for all threads)
 template <int N>
-__device__ __forceinline__ void to_runs(uint32_t (&q)[4][N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    swap_halves(q[0][i], q[2][i]);
-    swap_halves(q[1][i], q[3][i]);
-    const uint32_t t = q[1][i];
-    q[1][i] = q[2][i], q[2][i] = t;
-  }
-}
-template <int N>
-__device__ __forceinline__ void to_quads(uint32_t (&q)[4][N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const uint32_t t = q[1][i];
-    q[1][i] = q[2][i], q[2][i] = t;
-    swap_halves(q[0][i], q[2][i]);
-    swap_halves(q[1][i], q[3][i]);
-  }
-}
-// 32 features of row `p` on (`left` of them exist), stored where `in`
-__device__ __forceinline__ void store_feats(bf16 *p, int left, bool in, const float (&v)[16]) {
-  uint32_t q[4][2];
-#pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    q[g][0] = bf_pair(v[4 * g], v[4 * g + 1]);
-    q[g][1] = bf_pair(v[4 * g + 2], v[4 * g + 3]);
-  }
-  to_runs(q);
-  const int h = (threadIdx.x & 32) / 2;
-  p += h, left -= h;
-  if (!in) return;
-  if (left >= 16) {
-    *(u32x4_a2 *)p = (u32x4_a2){q[0][0], q[0][1], q[1][0], q[1][1]};
-    *(u32x4_a2 *)(p + 8) = (u32x4_a2){q[2][0], q[2][1], q[3][0], q[3][1]};
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (i < left) p[i] = (bf16)(q[i / 4][i / 2 % 2] >> (16 * (i & 1)));
-  }
-}
-__device__ __forceinline__ void store_feats(float *p, int left, bool in, const float (&v)[16]) {
-  uint32_t q[4][4];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) q[i / 4][i % 4] = __float_as_uint(v[i]);
-  to_runs(q);
-  const int h = (threadIdx.x & 32) / 2;
-  p += h, left -= h;
-  if (!in) return;
-#pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    if (left >= 4 * g + 4) {
-      *(f32x4_a4 *)(p + 4 * g) =
-          (f32x4_a4){__uint_as_float(q[g][0]), __uint_as_float(q[g][1]),
-                     __uint_as_float(q[g][2]), __uint_as_float(q[g][3])};
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (4 * g + i < left) p[4 * g + i] = __uint_as_float(q[g][i]);
-    }
-  }
-}
-// The same features read; zeros behind the last one
-__device__ __forceinline__ void load_feats(const bf16 *p, int left, float (&v)[16]) {
-  const int h = (threadIdx.x & 32) / 2;
-  const Raw8<bf16> a = load8(p + h, left - h), b = load8(p + h + 8, left - h - 8);
-  uint32_t q[4][2] = {{a.w[0], a.w[1]}, {a.w[2], a.w[3]}, {b.w[0], b.w[1]}, {b.w[2], b.w[3]}};
-  to_quads(q);
-#pragma unroll
-  for (int i = 0; i < 16; ++i)
-    v[i] = __uint_as_float(i & 1 ? q[i / 4][i / 2 % 2] & 0xffff0000u : q[i / 4][i / 2 % 2] << 16);
-}
-__device__ __forceinline__ void load_feats(const float *p, int left, float (&v)[16]) {
-  const int h = (threadIdx.x & 32) / 2;
-  float t[2][8];
-  load8(p + h, left - h).get(t[0]);
-  load8(p + h + 8, left - h - 8).get(t[1]);
-  uint32_t q[4][4];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) q[i / 4][i % 4] = __float_as_uint(t[i / 8][i % 8]);
-  to_quads(q);
-#pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(q[i / 4][i % 4]);
-}
-// A vector over the features (bias), the lane's own quads; zeros without one
-__device__ __forceinline__ void load_quads(const float *p, int left, float (&v)[16]) {
-  const int h = (threadIdx.x & 32) / 8;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int f = 8 * (i / 4) + h + i % 4;
-    v[i] = p && f < left ? p[f] : 0.f;
-  }
-}
-// The checkpoint's group of 32 features of a row: codes and exponent byte, by the
-// rules of encode8.
-__device__ __forceinline__ void put_feats(const Ckpt &k, int64_t row, int c, bool in,
-                                          const float (&v)[16]) {
-  uint32_t m = 0;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-  uint32_t o = m;
-  swap_halves(m, o);
-  m = max(m, o);
-  uint32_t E = max((m + 0x10000u) >> 23, 7u), q[4][1];
-  if (__builtin_expect(m >= 0x7f7f0000u, 0)) {
-    const bool bad = m >= 0x7f800000u;
-    E = bad ? 255u : 254u;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      q[g][0] = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float s = fminf(fmaxf(v[4 * g + i] * 0x1p-121f, -127.f), 127.f);
-        q[g][0] |= (bad ? 0 : __float_as_uint(s + 12582912.f) & 0xffu) << (8 * i);
-      }
-    }
-  } else {
-    const float inv = __uint_as_float((260u - E) << 23);
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      uint32_t b[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) b[i] = __float_as_uint(fmaf(v[4 * g + i], inv, 12582912.f));
-      q[g][0] = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u) |
-                __builtin_amdgcn_perm(b[3], b[2], 0x04000c0cu);
-    }
-  }
-  to_runs(q);
-  if (!in) return;
-  const int half = threadIdx.x & 32;
-  *(u32x4 *)(k.q + row * k.pitch + c + half / 2) = (u32x4){q[0][0], q[1][0], q[2][0], q[3][0]};
-  if (!half) k.e[row * (k.pitch / kGroup) + c / kGroup] = (uint8_t)E;
-}
-__device__ __forceinline__ void get_feats(const Ckpt &k, int64_t row, int c, float (&v)[16]) {
-  const u32x4 w = *(const u32x4 *)(k.q + row * k.pitch + c + (threadIdx.x & 32) / 2);
-  const float step = step_of(k.e[row * (k.pitch / kGroup) + c / kGroup]);
-  uint32_t q[4][1] = {{w.x}, {w.y}, {w.z}, {w.w}};
-  to_quads(q);
-#pragma unroll
-  for (int g = 0; g < 4; ++g) decode4(q[g][0], step, v + 4 * g);
-}
-
-// ----------------------------------------------------------- epilogues
-// f of the call's kind on 16 values (the same branch for all threads)
-__device__ __forceinline__ void activate16(int kind, const float (&u)[16], float (&f)[16],
-                                           float (&df)[16]) {
+__device__ __forceinline__ void activate_all(int kind, const float (&u)[N], float (&f)[N],
+                                             float (&df)[N]) {
   auto all = [&](auto K) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) activate<decltype(K)::value>(u[i], f[i], df[i]);
+    for (int i = 0; i < N; ++i) activate<decltype(K)::value>(u[i], f[i], df[i]);
   };
   using std::integral_constant;
   if (kind == LRCNN_ACT_SILU) all(integral_constant<int, LRCNN_ACT_SILU>());
@@ -208,60 +103,96 @@ __device__ __forceinline__ void activate16(int kind, const float (&u)[16], float
   else if (kind == LRCNN_ACT_GELU_TANH) all(integral_constant<int, LRCNN_ACT_GELU_TANH>());
   else all(integral_constant<int, LRCNN_ACT_RELU>());
 }
-// Features c .. c + 31 of a row from its accumulators: b0 (EPI_GATE: of u, and b1 of v)
-template <typename T, int EPI>
-__device__ __forceinline__ void finish(const FfnArgs &a, int row, int c, const float (&bias0)[16],
-                                       const float (&bias1)[16], const f32x16 &b0,
-                                       const f32x16 &b1) {
-  const bool in = row < a.rows;
-  const int64_t r = min(row, a.rows - 1);
-  const int left = a.feats - c;
-  if (left <= 0) return;
-  float f[16], df[16], u[16], v[16];
-  if constexpr (EPI == EPI_GATE) {
-    const int h = (threadIdx.x & 32) / 8;
+// A lane's eight features of a strip of FB blocks (EPI_GATE: blocks of u and v in turn)
+template <int EPI, int FB>
+struct Lanes {
+  static constexpr int WIDTH = 32 * FB / (EPI == EPI_GATE ? 2 : 1);  // features of a strip
+  static constexpr int PER = WIDTH / 8, ROWS = 64 / PER;             // lanes a row, rows a pass
+};
+struct Bias {
+  float u[8], v[8];
+  // of the features c .. c + 7
+  template <int EPI>
+  __device__ __forceinline__ void load(const FfnArgs &a, int c) {
+    const int n = a.feats - c;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const bool is = 8 * (i / 4) + h + i % 4 < left;
-      u[i] = is ? b0[i] + bias0[i] : 0.f;
-      v[i] = is ? b1[i] + bias1[i] : 0.f;
-    }
-    if (a.uv.p) {
-      T *p = (T *)a.uv.p + r * a.uv.ld + c;
-      store_feats(p, left, in, u);
-      store_feats(p + a.feats, left, in, v);
-    }
-    if (a.ku.q) put_feats(a.ku, r, c, in, u);
-    if (a.kv.q) put_feats(a.kv, r, c, in, v);
-    activate16(a.kind, u, f, df);
+    for (int i = 0; i < 8; ++i) u[i] = v[i] = 0.f;
+    if (EPI == EPI_BACK || !a.bias || n <= 0) return;
+    load8(a.bias + c, n).get(u);
+    if (EPI == EPI_GATE) load8(a.bias + a.feats + c, n).get(v);
+  }
+};
+// Rows r0 .. r0 + 31 and features c0 on from their strip. codes(row, u, v): EPI_BACK, u
+// and v of this lane's features of a row of the strip; all lanes call it.
+template <typename T, int EPI, int FB, typename Codes>
+__device__ __forceinline__ void strip_rows(const FfnArgs &a, lds_char *l, int r0, int c0,
+                                           const Bias &bias, Codes &&codes) {
+  typedef Lanes<EPI, FB> N;
+  const int lane = threadIdx.x & 63, k = lane % N::PER, c = c0 + 8 * k, n = a.feats - c;
+#pragma unroll 1
+  for (int p = 0; p < 32 / N::ROWS; ++p) {
+    const int row = p * N::ROWS + lane / N::PER;
+    const int64_t r = r0 + row;
+    float u[8], v[8], f[8], df[8];
+    if constexpr (EPI == EPI_BACK) codes(row, u, v);
+    // (the quad of a checkpoint's group goes on or stops as one)
+    if (r >= a.rows || n <= (EPI == EPI_PLAIN ? 0 : -(-a.feats & (kGroup - 1)))) continue;
+    if constexpr (EPI == EPI_GATE) {
+      const int slot = k / 4 * 16 + k % 4 * 2;
+      strip_get<FB>(l, row, slot, u);
+      strip_get<FB>(l, row, slot + 8, v);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) f[i] *= v[i];
-    store_feats((T *)a.out.p + r * a.out.ld + c, left, in, f);
-  } else if constexpr (EPI == EPI_BACK) {
-    if (a.uv.p) {
-      const T *p = (const T *)a.uv.p + r * a.uv.ld + c;
-      load_feats(p, left, u);
-      load_feats(p + a.feats, left, v);
+      for (int i = 0; i < 8; ++i) u[i] += bias.u[i], v[i] += bias.v[i];
+      if (n < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i >= n) u[i] = v[i] = 0.f;
+      }
+      if (a.uv.p) {
+        T *q = (T *)a.uv.p + r * a.uv.ld + c;
+        store8(q, n, u);
+        store8(q + a.feats, n, v);
+      }
+      if (a.ku.q) put8(a.ku, r, c, u);
+      if (a.kv.q) put8(a.kv, r, c, v);
+      activate_all(a.kind, u, f, df);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] *= v[i];
+      store8((T *)a.out.p + r * a.out.ld + c, n, f);
+    } else if constexpr (EPI == EPI_BACK) {
+      float d[8];
+      strip_get<FB>(l, row, 2 * k, d);
+      activate_all(a.kind, u, f, df);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        df[i] *= d[i] * v[i];
+        d[i] *= f[i];
+        f[i] *= v[i];
+      }
+      T *q = (T *)a.out.p + r * a.out.ld + c;
+      store8(q, n, df);
+      store8(q + a.feats, n, d);
+      if (a.ka.q) put8(a.ka, r, c, f);
     } else {
-      get_feats(a.ku, r, c, u);
-      get_feats(a.kv, r, c, v);
-    }
-    activate16(a.kind, u, f, df);
-    float du[16], dv[16];
+      strip_get<FB>(l, row, 2 * k, f);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      du[i] = b0[i] * df[i] * v[i];
-      dv[i] = b0[i] * f[i];
-      f[i] *= v[i];
+      for (int i = 0; i < 8; ++i) f[i] += bias.u[i];
+      store8((T *)a.out.p + r * a.out.ld + c, n, f);
     }
-    T *p = (T *)a.out.p + r * a.out.ld + c;
-    store_feats(p, left, in, du);
-    store_feats(p + a.feats, left, in, dv);
-    if (a.ka.q) put_feats(a.ka, r, c, in, f);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) f[i] = b0[i] + bias0[i];
-    store_feats((T *)a.out.p + r * a.out.ld + c, left, in, f);
+  }
+}
+// EPI_BACK: u and v of eight features from memory, zeros where there are none
+template <typename T>
+__device__ __forceinline__ void read_uv(const FfnArgs &a, int64_t r, int c, float (&u)[8],
+                                        float (&v)[8]) {
+  r = min(r, (int64_t)a.rows - 1);
+  if (a.uv.p) {
+    const T *q = (const T *)a.uv.p + r * a.uv.ld + c;
+    load8(q, a.feats - c).get(u);
+    load8(q + a.feats, a.feats - c).get(v);
+  } else if (c < a.ku.pitch) {
+    get8(a.ku, r, c, u);
+    get8(a.kv, r, c, v);
   }
 }
 
@@ -290,6 +221,7 @@ struct Tile {
   static constexpr int STAGE = (F + R) * kRow;
   static constexpr int SUMS = KS > 1 ? KS * FB * RB * 64 * 16 * 4 : 0;
   static constexpr int LDS = ST * STAGE > SUMS ? ST * STAGE : SUMS;
+  static_assert(LDS >= THREADS / 64 * 32 * 32 * FB * 4, "a strip for each wave");
 };
 
 // One step's products: fragments from an LDS stage. K order: lane half g takes the
@@ -324,6 +256,23 @@ __device__ __forceinline__ void products(const char *wt, const char *xt, int q, 
           acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(
               __uint_as_float(fw[i][e]), __uint_as_float(fx[j][e]), acc[i][j], 0, 0, 0);
   }
+}
+
+// 16 bytes a lane from global memory straight into LDS, lane l's to bytes 16 l of the
+// wave's address: as load16_lds_a, with the wait state between writing M0 and its
+// use by the copy that the GFX9 hazard rules ask for, which assembly has to keep by
+// itself. The second form takes a scalar base and a lane's offset from it.
+__device__ __forceinline__ void copy16(const void *p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"(lds), "v"(p)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void copy16(const char *base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(lds), "v"(off), "s"(base)
+               : "memory", "m0");
 }
 
 // DMA: rows of both operands at 16-byte steps from aligned bases and a depth of whole
@@ -394,7 +343,7 @@ __global__ __launch_bounds__(TL::THREADS) void ffn_kernel(FfnArgs a) {
 #pragma unroll
       for (int j = 0; j < NF + NR; ++j) {
         const int row = j < NF ? RP * j : TL::F + RP * (j - NF);
-        load16_lds_a(gp[j], ok, lds0 + st * TL::STAGE + (row + wave * 8) * kRow, zero);
+        copy16(ok ? gp[j] : (const char *)zero, lds0 + st * TL::STAGE + (row + wave * 8) * kRow);
         gp[j] += kRow;
       }
       kpos += BK;
@@ -454,10 +403,13 @@ __global__ __launch_bounds__(TL::THREADS) void ffn_kernel(FfnArgs a) {
       multiply(t & 1);
     }
   }
+  const int c0 = f0 + wf * Lanes<EPI, FB>::WIDTH;
+  Bias bias;
+  bias.load<EPI>(a, c0 + 8 * (lane % Lanes<EPI, FB>::PER));
+  __syncthreads();
   if constexpr (KS > 1) {
     // the waves' sums joined in order; wave j takes the blocks of rows j
     float *red = (float *)smem;
-    __syncthreads();
 #pragma unroll
     for (int i = 0; i < FB; ++i)
 #pragma unroll
@@ -466,33 +418,245 @@ __global__ __launch_bounds__(TL::THREADS) void ffn_kernel(FfnArgs a) {
         for (int v = 0; v < 16; ++v)
           red[(((wk * FB + i) * RB + j) * 16 + v) * 64 + lane] = acc[i][j][v];
     __syncthreads();
+    if (wave < RB) {
+#pragma unroll
+      for (int i = 0; i < FB; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          float s = 0.f;
+#pragma unroll
+          for (int k = 0; k < KS; ++k) s += red[(((k * FB + i) * RB + wave) * 16 + v) * 64 + lane];
+          acc[i][0][v] = s;
+        }
+    }
+    __syncthreads();
     if (wave >= RB) return;
-#pragma unroll
-    for (int i = 0; i < FB; ++i)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        float s = 0.f;
-#pragma unroll
-        for (int k = 0; k < KS; ++k) s += red[(((k * FB + i) * RB + wave) * 16 + v) * 64 + lane];
-        acc[i][0][v] = s;
-      }
   }
-  constexpr int STEP = EPI == EPI_GATE ? 2 : 1;
+  lds_char *const strip = (lds_char *)smem + wave * 32 * 32 * FB * 4;
+#pragma unroll 1
+  for (int j = 0; j < (KS > 1 ? 1 : RB); ++j) {
+    each<0, KS == 1 ? RB : 1>([&](auto j_) {
+      if (j == j_) each<0, FB>([&](auto i) { strip_put<FB>(strip, i, acc[i][j_]); });
+    });
+    wave_meets();
+    const int rj = r0 + 32 * (KS > 1 ? wave : wr * RB + j);
+    strip_rows<T, EPI, FB>(a, strip, rj, c0, bias, [&](int row, float (&u)[8], float (&v)[8]) {
+      read_uv<T>(a, rj + row, c0 + 8 * (lane % Lanes<EPI, FB>::PER), u, v);
+    });
+    wave_meets();
+  }
+}
+
+// Large products: 256 features by 256 rows, four waves of 128 x 128, one on each matrix
+// pipe. A wave reads (128 + 128) rows of fragments for 128 x 128 products; with
+// half-sized ones, eight to a tile, the LDS reads and the copies into it would take as
+// long as the products. Tile rows of 128 bytes (64 bfloat16 or 32 float32 of depth):
+// whole cache lines; with rows of 64 bytes and twice the stages the L2's requests bound it.
+//
+// A step has four slices of 16 bytes. Its order is laid down slot by slot, one block's
+// products to a slot: each slice reads the next one's fragments; before the last one
+// the waves meet -- the other stage has arrived, this one has been read by all -- and
+// during it the other stage's first fragments are read and this stage is copied over with
+// the step two ahead, which has the next step's first three slices to arrive. Past
+// the last step zeros are copied, so every step is alike.
+constexpr int kBigTile = 256, kBackPart = 40960;
+// Four neighbouring exponent bytes, of those that there are
+__device__ __forceinline__ uint32_t exponents4(const Ckpt &k, int64_t row, int c) {
+  typedef uint32_t u32_a1 __attribute__((aligned(1)));
+  const uint8_t *p = k.e + row * (k.pitch / kGroup) + c / kGroup;
+  const int64_t left = k.pitch - c;
+  if (left >= 4 * kGroup) return *(const u32_a1 *)p;
+  uint32_t e = 0;
 #pragma unroll
-  for (int i = 0; i < FB; i += STEP) {
-    const int c = f0 + (wf * FB + i) / STEP * 32;
-    float bias0[16], bias1[16];
-    if constexpr (EPI != EPI_BACK) load_quads(a.bias ? a.bias + c : nullptr, a.feats - c, bias0);
-    if constexpr (EPI == EPI_GATE)
-      load_quads(a.bias ? a.bias + a.feats + c : nullptr, a.feats - c, bias1);
-    if constexpr (KS > 1) {
-      finish<T, EPI>(a, r0 + 32 * wave + (lane & 31), c, bias0, bias1, acc[i][0],
-                     acc[i + STEP - 1][0]);
+  for (int i = 0; i < 4; ++i)
+    if (i * kGroup < left) e |= (uint32_t)p[i] << (8 * i);
+  return e;
+}
+template <typename T, int EPI>
+__global__ __launch_bounds__(256, 1) void ffn_big_kernel(FfnArgs a) {
+  constexpr int E = 16 / (int)sizeof(T), BK = kRow / (int)sizeof(T);
+  constexpr int STAGE = 2 * kBigTile * kRow, LD = 16;
+  __shared__ __align__(16) char smem[EPI == EPI_BACK ? 4 * kBackPart : 2 * STAGE];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int tx, ty;
+  tile_of(a, &tx, &ty);
+  const int r0 = tx * kBigTile, f0 = ty * (EPI == EPI_GATE ? kBigTile / 2 : kBigTile);
+  const int steps = (a.depth + BK - 1) / BK;
+  // rows tid / 8 + 32 j of each operand, one vector each, to slot tid % 8
+  const int br = tid >> 3, vec = (tid & 7) ^ ((tid >> 4) & 7);
+  uint32_t off[LD];
+  const int first = min(r0, a.rows - 1);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int t = br + 32 * j;
+    int64_t f;
+    if constexpr (EPI == EPI_GATE) {
+      const int h = f0 + t / 64 * 32 + (t & 31);  // blocks of u and v in turn
+      f = min(h, a.feats - 1) + ((t >> 5) & 1 ? (int64_t)a.feats : 0);
     } else {
+      f = min(f0 + t, a.feats - 1);
+    }
+    off[j] = (uint32_t)((f * a.depth + vec * E) * (int64_t)sizeof(T));
+    off[8 + j] = (uint32_t)(((int64_t)(min(r0 + t, a.rows - 1) - first) * a.x.ld + vec * E) *
+                            (int64_t)sizeof(T));
+  }
+  const char *gw = a.w, *gx = a.x.p + (int64_t)first * a.x.ld * (int64_t)sizeof(T);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem +
+                        wave * 8 * kRow;
+  int kpos = 0;  // of the step to copy
+  // WHOLE: the step's depth is there to its end
+  auto bring = [&](int st, int j, auto whole) {
+    const uint32_t to = lds0 + st * STAGE + 32 * kRow * j;
+    if constexpr (decltype(whole)::value) {
+      copy16(j < 8 ? gw : gx, off[j], to);
+    } else {
+      const bool ok = kpos + vec * E < a.depth;
+      copy16(ok ? (j < 8 ? gw : gx) + off[j] : (const char *)&g_zero16[0], to);
+    }
+  };
+  auto advance = [&]() {
+    kpos += BK, gw += kRow, gx += kRow;
+    asm volatile("" : "+s"(gw), "+s"(gx));
+  };
+  f32x16 acc[4][4];
 #pragma unroll
-      for (int j = 0; j < RB; ++j)
-        finish<T, EPI>(a, r0 + 32 * (wr * RB + j) + (lane & 31), c, bias0, bias1, acc[i][j],
-                       acc[i + STEP - 1][j]);
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+  const int wf = wave & 1, wr = wave >> 1;
+  typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+  lds_char *lds = (lds_char *)smem;
+  // a fragment of slice q: vector 4 (lane / 32) + q of row lane % 32 of its block
+  int pw[4], px[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int r = lane & 31, at = r * kRow + swz<8>(r, 4 * (lane >> 5) + q) * 16;
+    pw[q] = at + wf * 128 * kRow;
+    px[q] = at + (kBigTile + wr * 128) * kRow;
+  }
+  u32x4 fw[2][4], fx[2][4];
+  // fragment k of slice q: the first weights', the rows', then the other weights'
+  auto fragment = [&](int st, auto q_, auto k_) {
+    constexpr int q = decltype(q_)::value, k = decltype(k_)::value, p = q & 1;
+    if constexpr (k == 0) fw[p][0] = *(lds_u32x4 *)(lds + st * STAGE + pw[q]);
+    else if constexpr (k < 5)
+      fx[p][k - 1] = *(lds_u32x4 *)(lds + st * STAGE + px[q] + (k - 1) * 32 * kRow);
+    else fw[p][k - 4] = *(lds_u32x4 *)(lds + st * STAGE + pw[q] + (k - 4) * 32 * kRow);
+  };
+  using std::integral_constant;
+  // slice q of the step on stage st
+  auto slice = [&](auto q_, int st, auto whole) {
+    constexpr int q = decltype(q_)::value, p = q & 1;
+    each<0, 16>([&](auto m_) {
+      constexpr int m = decltype(m_)::value, i = m / 4, j = m % 4;
+      if constexpr (sizeof(T) == 2) {
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fw[p][i]),
+                                                            __builtin_bit_cast(bf16x8, fx[p][j]),
+                                                            acc[i][j], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fw[p][i][e]),
+                                                           __uint_as_float(fx[p][j][e]),
+                                                           acc[i][j], 0, 0, 0);
+      }
+      if constexpr (m < 8) fragment(q == 3 ? st ^ 1 : st, integral_constant<int, (q + 1) % 4>(), m_);
+      if constexpr (q == 3) bring(st, m, whole);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  auto step = [&](int st, auto whole) {
+    slice(integral_constant<int, 0>(), st, whole);
+    slice(integral_constant<int, 1>(), st, whole);
+    slice(integral_constant<int, 2>(), st, whole);
+    wait_vmcnt<0>();
+    __syncthreads();
+    slice(integral_constant<int, 3>(), st, whole);
+    advance();
+  };
+  for (int i = 0; i < 2; ++i) {
+#pragma unroll
+    for (int j = 0; j < LD; ++j) bring(i, j, std::false_type());
+    advance();
+  }
+  wait_vmcnt<LD>();
+  __syncthreads();
+  each<0, 8>([&](auto k) { fragment(0, integral_constant<int, 0>(), k); });
+  int t = 0;
+  for (; kpos + BK <= a.depth; ++t) step(t & 1, std::true_type());
+  for (; t < steps; ++t) step(t & 1, std::false_type());
+  wait_vmcnt<0>();
+  const int wrow = r0 + wr * 128;
+  if constexpr (EPI != EPI_BACK) {
+    const int c0 = f0 + wf * Lanes<EPI, 4>::WIDTH;
+    Bias bias;
+    bias.load<EPI>(a, c0 + 8 * (lane % Lanes<EPI, 4>::PER));
+    __syncthreads();
+    lds_char *const strip = (lds_char *)smem + wave * 32 * 128 * 4;
+#pragma unroll 1
+    for (int j = 0; j < 4; ++j) {
+      each<0, 4>([&](auto j_) {
+        if (j == j_) each<0, 4>([&](auto i) { strip_put<4>(strip, i, acc[i][j_]); });
+      });
+      wave_meets();
+      strip_rows<T, EPI, 4>(a, strip, wrow + 32 * j, c0, bias,
+                            [](int, float (&)[8], float (&)[8]) {});
+      wave_meets();
+    }
+  } else {
+    // This wave's LDS: a strip of 64 features, then the codes of u and v, 4 KB of
+    // each for 32 rows of 128 features. They are all on their way before the first
+    // store, as a wait for a load waits for the stores before it.
+    const int c0 = f0 + wf * 128;
+    lds_char *const strip = (lds_char *)smem + wave * kBackPart, *const held = strip + 8192;
+    __syncthreads();
+    const bool ck = a.ku.q != nullptr;
+    uint32_t eu[2] = {0, 0}, ev[2] = {0, 0};  // exponents of rows lane and lane + 64
+    if (ck && c0 < a.feats) {
+#pragma unroll 4
+      for (int i = 0; i < 16; ++i) {
+        const int row = 8 * i + lane / 8, c = c0 + ((lane & 7) ^ (row & 7)) * 16;
+        const int64_t r = min(wrow + row, a.rows - 1);
+        const bool ok = c < a.ku.pitch;
+        const uint32_t to = (uint32_t)(uintptr_t)held + (i / 4 * 8 + i % 4) * 1024;
+        const char *const zero = (const char *)&g_zero16[0];
+        copy16(ok ? (const char *)a.ku.q + r * a.ku.pitch + c : zero, to);
+        copy16(ok ? (const char *)a.kv.q + r * a.kv.pitch + c : zero, to + 4096);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int64_t r = min(wrow + 64 * h + lane, a.rows - 1);
+        eu[h] = exponents4(a.ku, r, c0);
+        ev[h] = exponents4(a.kv, r, c0);
+      }
+      wait_vmcnt<0>();
+    }
+#pragma unroll 1
+    for (int jh = 0; jh < 8; ++jh) {
+      each<0, 8>([&](auto x) {
+        constexpr int j = decltype(x)::value / 2, h = decltype(x)::value % 2;
+        if (jh == x)
+          each<0, 2>([&](auto i) { strip_put<2>(strip, i, acc[2 * h + i][j]); });
+      });
+      wave_meets();
+      const int j = jh >> 1, h = jh & 1, rj = wrow + 32 * j;
+      const uint32_t wu = j < 2 ? eu[0] : eu[1], wv = j < 2 ? ev[0] : ev[1];
+      strip_rows<T, EPI, 2>(
+          a, strip, rj, c0 + 64 * h, Bias(), [&](int row, float (&u)[8], float (&v)[8]) {
+            const int k = lane & 7;
+            if (ck) {
+              const int at = j * 8192 + row * 128 + ((4 * h + k / 2) ^ (row & 7)) * 16 + k % 2 * 8;
+              const int from = (32 * j + row) & 63, by = 8 * (2 * h + k / 4);
+              decode8(lds_pair(held + at), (__shfl(wu, from) >> by) & 255u, u);
+              decode8(lds_pair(held + at + 4096), (__shfl(wv, from) >> by) & 255u, v);
+            } else {
+              read_uv<T>(a, rj + row, c0 + 64 * h + 8 * k, u, v);
+            }
+          });
+      wave_meets();
     }
   }
 }
@@ -607,19 +771,22 @@ __global__ __launch_bounds__(512) void ffn_few_kernel(FfnArgs a) {
 }
 
 // ------------------------------------------------------------- launches
-typedef Tile<4, 2, 2, 4, 1, 2> Big;    // 256 features x 256 rows, 8 waves
 typedef Tile<2, 2, 2, 2, 1, 2> Mid;    // 128 x 128, 4 waves
 typedef Tile<1, 2, 1, 2, 4, 3> Small;  // 64 x 64, 4 waves that split the depth
 constexpr int kFewRows = 32;
 
-template <typename T, typename TL, int EPI, bool DMA>
-int launch(FfnArgs &a, hipStream_t s) {
-  constexpr int F = EPI == EPI_GATE ? TL::F / 2 : TL::F;
-  a.gx = (a.rows + TL::R - 1) / TL::R;
-  a.gy = (a.feats + F - 1) / F;
+int lay_out(FfnArgs &a, int rows, int feats) {
+  a.gx = (a.rows + rows - 1) / rows;
+  a.gy = (a.feats + feats - 1) / feats;
   if ((int64_t)a.gx * a.gy > 1 << 22) return refuse(LRCNN_ESHAPE, "gated_ffn: too many tiles");
   a.panel = fast_div(8 * (uint32_t)a.gy);
   a.rest = fast_div((uint32_t)std::max(a.gx & 7, 1));
+  return LRCNN_OK;
+}
+template <typename T, typename TL, int EPI, bool DMA>
+int launch(FfnArgs &a, hipStream_t s) {
+  const int st = lay_out(a, TL::R, EPI == EPI_GATE ? TL::F / 2 : TL::F);
+  if (st != LRCNN_OK) return st;
   ffn_kernel<T, TL, EPI, DMA><<<(unsigned)(a.gx * a.gy), TL::THREADS, 0, s>>>(a);
   return LRCNN_OK;
 }
@@ -644,8 +811,14 @@ int product(FfnArgs a, hipStream_t s) {
   if (tiles(Mid::F, Mid::R) < 256)
     return dma ? launch<T, Small, EPI, true>(a, s) : launch<T, Small, EPI, false>(a, s);
   if (!dma) return launch<T, Mid, EPI, false>(a, s);
-  if (tiles(Big::F, Big::R) < 256) return launch<T, Mid, EPI, true>(a, s);
-  return launch<T, Big, EPI, true>(a, s);
+  // (the large tile's copies have 32-bit offsets)
+  const bool near = (int64_t)a.feats * H * a.depth * (int64_t)sizeof(T) < (int64_t)1 << 32 &&
+                    kBigTile * a.x.ld * (int64_t)sizeof(T) < (int64_t)1 << 32;
+  if (!near || tiles(kBigTile, kBigTile) < 256) return launch<T, Mid, EPI, true>(a, s);
+  const int st = lay_out(a, kBigTile, kBigTile / H);
+  if (st != LRCNN_OK) return st;
+  ffn_big_kernel<T, EPI><<<(unsigned)(a.gx * a.gy), 256, 0, s>>>(a);
+  return LRCNN_OK;
 }
 
 template <int EPI>
