@@ -215,6 +215,18 @@ __device__ __forceinline__ void store8(float *p, int64_t n, const float (&v)[8])
   }
 }
 
+// 1 / sqrt(x) to the last bit but for near ties: the instruction's value, an ulp off
+// in one row of seven (an error that a whole row and its checkpoint share), and
+// one Newton step y + y (1 - x y^2) / 2, x y as a sum of two floats. Zero and
+// infinity, where the step is NaN, keep their limits.
+__device__ __forceinline__ float rsqrt_rounded(float x) {
+  const float y = rsqrtf(x);
+  const float h = x * y, l = fmaf(x, y, -h);
+  const float e = fmaf(-l, y, fmaf(-h, y, 1.f));
+  const float z = fmaf(0.5f * e, y, y);
+  return z == z ? z : y;
+}
+
 // ------------------------------------------------------------- the codes
 // quad_perm moves inside the four lanes that hold one group
 __device__ __forceinline__ uint32_t quad_max(uint32_t m) {

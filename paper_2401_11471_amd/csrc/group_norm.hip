@@ -20,6 +20,7 @@
 // so that a mean far from zero costs the variance no digits; across slabs
 // and channels in 64 bits.
 #include "activation.hpp"
+#include "kernels.hpp"
 
 #include <algorithm>
 #include <type_traits>
@@ -30,6 +31,7 @@ namespace {
 
 constexpr int64_t kMaxImages = 1 << 20, kMaxChannels = 1 << 20;
 constexpr int kBatch = 8;         // pixels that a thread holds at a time
+constexpr int kLeast = 2;         // pixels a thread, where that gives the CUs work
 constexpr int kUnits = 2048;      // blocks of a pass, where there are as many
 constexpr int kApplyPixels = 4;   // applying passes: pixels in flight a thread
 
@@ -39,6 +41,7 @@ struct GnArgs {
   int slabs, batch, cols, pitch, groups, per;  // per: channels of a group
   int tpr, ctiles;       // threads of a pixel's channels; tiles of 8 tpr channels
   float eps;
+  double inv;            // 1 / (pixels of an image times channels of a group)
   Mat x, y;              // backward: y is dy
   Mat dx;
   const float *gamma, *beta;
@@ -48,6 +51,8 @@ struct GnArgs {
   float2 *stat;          // [batch][groups]: (mean, rstd), backward the two means
   float *dgamma, *dbeta;
   int accumulate;
+  FastDiv by_per;
+  int width;             // channels of a block that holds its groups whole
   Ckpt k;
 };
 
@@ -57,10 +62,14 @@ struct Place {
   int64_t unit;
   int c, n, row, rows;  // first channel, channels left, this thread's row and rows a block
 };
+// BACK: the units from the last one on, in the second pass: it begins with what the first
+// one left in the Infinity Cache.
+template <bool BACK = false>
 __device__ __forceinline__ Place place(const GnArgs &a) {
   Place q;
-  const int ct = blockIdx.x % a.ctiles;
-  q.unit = blockIdx.x / a.ctiles;
+  const uint32_t block = BACK ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
+  const int ct = block % a.ctiles;
+  q.unit = block / a.ctiles;
   q.b = q.unit / a.slabs;
   q.p0 = (q.unit - q.b * a.slabs) * a.slab;
   q.p1 = min(q.p0 + a.slab, a.pixels);
@@ -196,31 +205,38 @@ __device__ __forceinline__ double block_sum(double v, double *red) {
 }
 
 // Block (image, group): mean and rstd of a group from its slabs' channels
-__global__ __launch_bounds__(256) void gn_group_kernel(GnArgs a) {
-  __shared__ double red[4];
+__global__ __launch_bounds__(1024) void gn_group_kernel(GnArgs a) {
+  __shared__ double red[16];
   const int64_t b = blockIdx.x / a.groups;
   const int g = blockIdx.x % a.groups;
-  const int64_t all = (int64_t)a.slabs * a.per;
+  const uint32_t all = (uint32_t)a.slabs * (uint32_t)a.per;
   const float2 *part = a.part + b * a.slabs * (int64_t)a.cols + (int64_t)g * a.per;
-  const double total = (double)a.pixels * a.per;
-  auto count = [&](int64_t s) { return (double)min(a.slab, a.pixels - s * a.slab); };
+  auto count = [&](uint32_t s) { return (double)min(a.slab, a.pixels - s * a.slab); };
+  auto at = [&](uint32_t e, uint32_t &s) {
+    uint32_t c;
+    fdiv_qr(e, a.by_per, s, c);
+    return part[(int64_t)s * a.cols + c];
+  };
   double sum = 0;
-  for (int64_t e = threadIdx.x; e < all; e += 256) {
-    const int64_t s = e / a.per;
-    sum += count(s) * part[s * a.cols + (e - s * a.per)].x;
+#pragma unroll 4
+  for (uint32_t e = threadIdx.x; e < all; e += 1024) {
+    uint32_t s;
+    const float2 v = at(e, s);
+    sum += count(s) * v.x;
   }
-  const double mean = block_sum(sum, red) / total;
+  const double mean = block_sum(sum, red) * a.inv;
   double m2 = 0;
-  for (int64_t e = threadIdx.x; e < all; e += 256) {
-    const int64_t s = e / a.per;
-    const float2 v = part[s * a.cols + (e - s * a.per)];
+#pragma unroll 4
+  for (uint32_t e = threadIdx.x; e < all; e += 1024) {
+    uint32_t s;
+    const float2 v = at(e, s);
     const double d = v.x - mean;
     m2 += v.y + count(s) * d * d;
   }
-  double var = block_sum(m2, red) / total;
+  double var = block_sum(m2, red) * a.inv;
   var = var < 0 ? 0 : var;  // (NaN stays)
   if (threadIdx.x == 0) {
-    const float m = (float)mean, r = (float)(1 / sqrt(var + (double)a.eps));
+    const float m = (float)mean, r = rsqrt_rounded((float)var + a.eps);
     a.stat[blockIdx.x] = make_float2(m, r);
     if (a.mean_out) a.mean_out[blockIdx.x] = m;
     if (a.rstd_out) a.rstd_out[blockIdx.x] = r;
@@ -229,7 +245,7 @@ __global__ __launch_bounds__(256) void gn_group_kernel(GnArgs a) {
 
 template <typename T, int KIND>
 __global__ __launch_bounds__(256) void gn_apply_kernel(GnArgs a) {
-  const Place q = place(a);
+  const Place q = place<true>(a);
   if (q.c >= a.pitch) return;
   float ga[8], be[8], mu[8], rs[8];
   channel8(a.gamma, q, 1.f, ga);
@@ -362,32 +378,11 @@ __global__ __launch_bounds__(256) void gn_sums_kernel(GnArgs a) {
   }
 }
 
-// The first batch * groups blocks: a group's two means, of q and q xh. Then one
-// block for 32 channels: dgamma and dbeta, thread (r, c) taking every 32nd unit
-// from r on, the 32 sums joined in order.
-__global__ __launch_bounds__(1024) void gn_join_kernel(GnArgs a) {
-  __shared__ double red[16];
+// dgamma and dbeta of 32 channels: thread (r, c) takes every 32nd unit from r on, the
+// 32 sums joined in order.
+__device__ __forceinline__ void channel_grads(const GnArgs &a, int block) {
   __shared__ float l1[32][33], l2[32][33];
-  const int64_t bg = (int64_t)a.batch * a.groups;
-  if (blockIdx.x < bg) {
-    const int64_t b = blockIdx.x / a.groups;
-    const int g = blockIdx.x % a.groups;
-    const int64_t all = (int64_t)a.slabs * a.per;
-    const float2 *part = a.part + b * a.slabs * (int64_t)a.cols + (int64_t)g * a.per;
-    double s1 = 0, s2 = 0;
-    for (int64_t e = threadIdx.x; e < all; e += 1024) {
-      const int64_t s = e / a.per, c = e - s * a.per;
-      const float2 v = part[s * a.cols + c];
-      const double ga = a.gamma ? (double)a.gamma[g * a.per + c] : 1.0;
-      s1 += ga * v.x, s2 += ga * v.y;
-    }
-    const double total = (double)a.pixels * a.per;
-    s1 = block_sum(s1, red);
-    s2 = block_sum(s2, red);
-    if (threadIdx.x == 0) a.stat[blockIdx.x] = make_float2((float)(s1 / total), (float)(s2 / total));
-    return;
-  }
-  const int r = threadIdx.x >> 5, c = (int)(blockIdx.x - bg) * 32 + (threadIdx.x & 31);
+  const int r = threadIdx.x >> 5, c = block * 32 + (threadIdx.x & 31);
   float s1 = 0.f, s2 = 0.f;
   if (c < a.cols) {
 #pragma unroll 8
@@ -405,11 +400,38 @@ __global__ __launch_bounds__(1024) void gn_join_kernel(GnArgs a) {
     if (a.dgamma) a.dgamma[c] = a.accumulate ? a.dgamma[c] + s2 : s2;
   }
 }
+__global__ __launch_bounds__(1024) void gn_grads_kernel(GnArgs a) {
+  channel_grads(a, blockIdx.x);
+}
+
+// Block (image, group): a group's two means, of q and q xh; the blocks behind these:
+// the parameters' gradients of 32 channels each.
+__global__ __launch_bounds__(1024) void gn_join_kernel(GnArgs a) {
+  __shared__ double red[16];
+  const int bg = a.batch * a.groups;
+  if ((int)blockIdx.x >= bg) return channel_grads(a, blockIdx.x - bg);
+  const int64_t b = blockIdx.x / a.groups;
+  const int g = blockIdx.x % a.groups;
+  const uint32_t all = (uint32_t)a.slabs * (uint32_t)a.per;
+  const float2 *part = a.part + b * a.slabs * (int64_t)a.cols + (int64_t)g * a.per;
+  double s1 = 0, s2 = 0;
+#pragma unroll 4
+  for (uint32_t e = threadIdx.x; e < all; e += 1024) {
+    uint32_t s, c;
+    fdiv_qr(e, a.by_per, s, c);
+    const float2 v = part[(int64_t)s * a.cols + c];
+    const double ga = a.gamma ? (double)a.gamma[g * a.per + c] : 1.0;
+    s1 += ga * v.x, s2 += ga * v.y;
+  }
+  s1 = block_sum(s1, red);
+  s2 = block_sum(s2, red);
+  if (threadIdx.x == 0) a.stat[blockIdx.x] = make_float2((float)(s1 * a.inv), (float)(s2 * a.inv));
+}
 
 template <typename T, int KIND, bool CK>
 __global__ __launch_bounds__(256) void gn_dx_kernel(GnArgs a) {
   constexpr int R = kApplyPixels;
-  const Place q = place(a);
+  const Place q = place<true>(a);
   if (q.n <= 0) return;
   Back<T, KIND, CK> back;
   back.init(a, q);
@@ -436,12 +458,253 @@ __global__ __launch_bounds__(256) void gn_dx_kernel(GnArgs a) {
   }
 }
 
+// ------------------------------------------------- maps that a block can hold
+// One pass: a block has some whole groups of an image, all their pixels in registers
+// (R a thread). `width` channels from its first on, eight to a thread; threads past the
+// width or the pixels hold zeros.
+struct Whole {
+  int64_t b;
+  int c0, c, n, row, rows;  // first channel of the block, of the thread; channels left
+};
+__device__ __forceinline__ Whole whole(const GnArgs &a) {
+  Whole w;
+  w.b = blockIdx.x / a.ctiles;
+  w.c0 = (int)(blockIdx.x % a.ctiles) * a.width;
+  const int k = threadIdx.x % a.tpr * kVec;
+  w.c = w.c0 + k;
+  w.n = min(a.width - k, a.cols - w.c);
+  w.row = threadIdx.x / a.tpr, w.rows = blockDim.x / a.tpr;
+  return w;
+}
+// Sums of M values a channel over the block's rows, then over each group's channels
+// weighted by `weigh`, of the channel within the block. chan [waves][M][8 tpr]: each channel's sums of a wave; the
+// waves and channels are added in 64 bits, by 16 threads a group, the first of which
+// makes of them what all threads find in stat[local group] (64-bit division and roots
+// by every thread take longer than the rest of a small call).
+constexpr int kWide = 512;  // channels of a block at most
+template <int M, typename F, typename G>
+__device__ __forceinline__ void group_sums(const GnArgs &a, const Whole &w, float (&v)[M][8],
+                                           float *chan, float2 *stat, F &&weigh, G &&make) {
+  const int wide = a.tpr * kVec;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  for (int s = a.tpr; s < 64; s *= 2) {  // (all values at a step: a move takes a while)
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[m][i] += __shfl_xor(v[m][i], s);
+  }
+  __syncthreads();
+  if (lane < a.tpr) {
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) chan[(wave * M + m) * wide + lane * 8 + i] = v[m][i];
+  }
+  __syncthreads();
+  const int here = min(a.width, a.cols - w.c0) / a.per;
+  const int all = waves * a.per;
+  for (int g = threadIdx.x >> 4; g < here; g += blockDim.x >> 4) {
+    double t[M];
+#pragma unroll
+    for (int m = 0; m < M; ++m) t[m] = 0;
+#pragma unroll 4
+    for (int e = threadIdx.x & 15; e < all; e += 16) {
+      uint32_t wv, c;
+      fdiv_qr((uint32_t)e, a.by_per, wv, c);
+      const int ch = g * a.per + (int)c;
+      const double wt = weigh(ch);
+#pragma unroll
+      for (int m = 0; m < M; ++m) t[m] += wt * chan[(wv * M + m) * wide + ch];
+    }
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+      for (int s = 1; s < 16; s *= 2) t[m] += __shfl_xor(t[m], s);
+    if ((threadIdx.x & 15) == 0) make(g, t);
+  }
+  __syncthreads();
+}
+// A thread's channels' local groups
+__device__ __forceinline__ int local_group(const GnArgs &a, const Whole &w, int i) {
+  return (int)fdiv_q((uint32_t)(min(w.c + i, w.c0 + min(a.width, a.cols - w.c0) - 1) - w.c0),
+                     a.by_per);
+}
+
+// Keeps the eight columns as they are stored: converted ones, kept for a later use, take
+// twice the registers.
+__device__ __forceinline__ void as_stored(Raw8<bf16> &r) { asm volatile("" : "+v"(r.w)); }
+__device__ __forceinline__ void as_stored(Raw8<float> &) {}
+
+template <typename T, int KIND, int R>
+__global__ __launch_bounds__(1024) void gn_whole_kernel(GnArgs a) {
+  extern __shared__ float2 stat[];  // [8 tpr], then chan (and, backward, gamma)
+  const int wide = a.tpr * kVec;
+  float *const chan = (float *)(stat + wide);
+  const Whole w = whole(a);
+  Raw8<T> r[R];
+  float v[2][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[0][i] = v[1][i] = 0.f;
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    const int64_t p = w.row + (int64_t)j * w.rows;
+    const bool in = p < a.pixels;
+    r[j] = load8((const T *)a.x.p + (w.b * a.pixels + (in ? p : 0)) * a.x.ld + w.c, in ? w.n : 0);
+  }
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    float x[8];
+    r[j].get(x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[0][i] += x[i];
+  }
+  auto one = [](int) { return 1.0; };
+  {
+    float t[1][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[0][i] = v[0][i];
+    group_sums<1>(a, w, t, chan, stat, one, [&](int g, const double (&t)[1]) {
+      stat[g].x = (float)(t[0] * a.inv);
+    });
+  }
+  int lg[8];
+  float mu[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    lg[i] = local_group(a, w, i);
+    mu[i] = stat[lg[i]].x;
+    v[0][i] = 0.f;
+  }
+  // the centred values' own sum corrects the mean
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    as_stored(r[j]);
+    const bool in = w.row + (int64_t)j * w.rows < a.pixels;
+    float x[8];
+    r[j].get(x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float d = in && i < w.n ? x[i] - mu[i] : 0.f;
+      v[0][i] += d;
+      v[1][i] = fmaf(d, d, v[1][i]);
+    }
+  }
+  group_sums<2>(a, w, v, chan, stat, one, [&](int g, const double (&t)[2]) {
+    const double off = t[0] * a.inv;
+    double var = t[1] * a.inv - off * off;
+    var = var < 0 ? 0 : var;  // (NaN stays)
+    const float2 s = make_float2((float)((double)stat[g].x + off),
+                                 rsqrt_rounded((float)var + a.eps));
+    stat[g] = s;
+    const int64_t at = w.b * a.groups + w.c0 / a.per + g;
+    if (a.mean_out) a.mean_out[at] = s.x;
+    if (a.rstd_out) a.rstd_out[at] = s.y;
+  });
+  float ga[8], be[8], rs[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float2 s = stat[lg[i]];
+    mu[i] = s.x, rs[i] = s.y;
+    ga[i] = 1.f, be[i] = 0.f;
+  }
+  if (a.gamma && w.n > 0) load8(a.gamma + w.c, w.n).get(ga);
+  if (a.beta && w.n > 0) load8(a.beta + w.c, w.n).get(be);
+  // (with a checkpoint the block's channels start and end with its groups of 32)
+  if (w.c >= (a.k.q ? min(a.pitch, w.c0 + (int)((a.width + kGroup - 1) / kGroup * kGroup)) : w.c0 + a.width)) return;
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    const int64_t p = w.row + (int64_t)j * w.rows;
+    if (p >= a.pixels) continue;
+    const int64_t at = w.b * a.pixels + p;
+    float x[8], y[8], df;
+    as_stored(r[j]);
+    r[j].get(x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[i] = i < w.n ? (x[i] - mu[i]) * rs[i] : 0.f;
+      activate<KIND>(fmaf(x[i], ga[i], be[i]), y[i], df);
+    }
+    if (w.n > 0) store8((T *)a.y.p + at * a.y.ld + w.c, w.n, y);
+    if (a.k.q) put8(a.k, at, w.c, x);
+  }
+}
+
+template <typename T, int KIND, bool CK, int R>
+__global__ __launch_bounds__(1024) void gn_whole_back_kernel(GnArgs a) {
+  extern __shared__ float2 stat[];  // [8 tpr], then chan (and, backward, gamma)
+  const int wide = a.tpr * kVec;
+  float *const chan = (float *)(stat + wide);
+  const Whole w = whole(a);
+  Place q;  // as Back reads it
+  q.b = w.b, q.c = w.c, q.n = w.n;
+  Back<T, KIND, CK> back;
+  back.init(a, q);
+  float xh[R][8], e[R][8], v[2][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[0][i] = v[1][i] = 0.f;
+  typename Back<T, KIND, CK>::Raw r[R];
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    const int64_t p = w.row + (int64_t)j * w.rows;
+    if (w.n > 0) r[j] = back.load(a, q, w.b * a.pixels + min(p, a.pixels - 1));
+  }
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    const bool in = w.row + (int64_t)j * w.rows < a.pixels && w.n > 0;
+    if (in) back.get(q, r[j], xh[j], e[j]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (in && i < w.n) {
+        v[0][i] += e[j][i];
+        v[1][i] = fmaf(e[j][i], xh[j][i], v[1][i]);
+      }
+  }
+  float *const gam = chan + (blockDim.x >> 6) * 2 * wide;
+  if (w.row == 0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) gam[w.c - w.c0 + i] = back.ga[i];
+  }
+  group_sums<2>(a, w, v, chan, stat, [&](int c) { return (double)gam[c]; },
+                [&](int g, const double (&t)[2]) {
+                  stat[g] = make_float2((float)(t[0] * a.inv), (float)(t[1] * a.inv));
+                });
+  // the image's sums of each channel, for dgamma and dbeta
+  if (a.part) {
+    const int waves = blockDim.x >> 6, here = min(a.width, a.cols - w.c0);
+    for (int c = threadIdx.x; c < here; c += blockDim.x) {
+      float s1 = 0.f, s2 = 0.f;
+      for (int k = 0; k < waves; ++k) s1 += chan[2 * k * wide + c], s2 += chan[(2 * k + 1) * wide + c];
+      if (a.batch == 1) {
+        const int at = w.c0 + c;
+        if (a.dbeta) a.dbeta[at] = a.accumulate ? a.dbeta[at] + s1 : s1;
+        if (a.dgamma) a.dgamma[at] = a.accumulate ? a.dgamma[at] + s2 : s2;
+      } else {
+        a.part[w.b * a.cols + w.c0 + c] = make_float2(s1, s2);
+      }
+    }
+  }
+  if (w.n <= 0) return;
+  float m1[8], m2[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float2 m = stat[local_group(a, w, i)];
+    m1[i] = m.x, m2[i] = m.y;
+  }
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    const int64_t p = w.row + (int64_t)j * w.rows;
+    if (p >= a.pixels) continue;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      e[j][i] = back.rs[i] * (fmaf(e[j][i], back.ga[i], -m1[i]) - xh[j][i] * m2[i]);
+    store8((T *)a.dx.p + (w.b * a.pixels + p) * a.dx.ld + w.c, w.n, e[j]);
+  }
+}
+
 // ------------------------------------------------------------------- plan
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 struct Split {
   int tpr, ctiles;
   int64_t slabs, slab;
-  int64_t most_units;  // of any call with as many images and pixels, or fewer
 };
 Split split_of(int64_t batch, int64_t pixels, int64_t cols) {
   Split s;
@@ -449,21 +712,54 @@ Split split_of(int64_t batch, int64_t pixels, int64_t cols) {
   s.tpr = 4;
   while (s.tpr < 64 && s.tpr < vecs) s.tpr *= 2;
   s.ctiles = (int)up(vecs, s.tpr);
-  const int64_t least = 256 / s.tpr * kBatch;  // pixels worth a block
+  pixels = std::max<int64_t>(pixels, 1);
+  const int64_t by_pixels = up(pixels, 256 / s.tpr * kLeast);  // pixels worth a block
   const int64_t units = std::max<int64_t>(kUnits / s.ctiles, 1);
-  const int64_t by_pixels = up(std::max<int64_t>(pixels, 1), least);
-  const int64_t n = std::max<int64_t>(std::min(units / std::max<int64_t>(batch, 1), by_pixels), 1);
-  s.slab = up(std::max<int64_t>(pixels, 1), n);
-  s.slabs = up(std::max<int64_t>(pixels, 1), s.slab);
-  s.most_units = std::max(batch, by_pixels >= units ? units : std::min(units, batch * by_pixels));
+  s.slab = up(pixels, std::max<int64_t>(
+                          std::min(units / std::max<int64_t>(batch, 1), by_pixels), 1));
+  s.slabs = up(pixels, s.slab);
   return s;
 }
-
-size_t part_bytes(const Split &s, int64_t cols) {
-  return a256((size_t)s.most_units * (size_t)cols * 8);
+// Never fewer units than split_of makes of as many images or fewer
+int64_t most_units(int64_t batch, int64_t cols) {
+  return std::max<int64_t>(batch, kUnits / split_of(1, 1, cols).ctiles);
 }
-size_t need_bytes(const Split &s, int64_t batch, int64_t cols, int64_t groups) {
-  return part_bytes(s, cols) + a256((size_t)batch * (size_t)groups * 8);
+
+// The block of a call whose groups fit into one: whole groups, at least 64 bytes of
+// a pixel, few idle lanes, where there is a checkpoint whole groups of 32 channels (or all
+// channels); pixels a thread R. width 0: they do not fit.
+struct Block {
+  int width = 0, tpr = 0, threads = 0, r = 0;
+};
+Block block_of(int64_t batch, int64_t pixels, int64_t cols, int64_t per, int es, bool ckpt,
+               int most_r) {
+  Block best;
+  double score = 0;
+  for (int64_t w = per; w <= cols && w <= kWide; w += per) {
+    if (ckpt && w % kGroup && w != cols) continue;
+    int tpr = 4;
+    while (tpr * kVec < w) tpr *= 2;
+    if (pixels > (int64_t)most_r * (1024 / tpr)) break;
+    const double line = std::min(1.0, (double)w * es / 64), full = (double)w / (tpr * kVec);
+    if (line * full <= score + 0.1) continue;
+    score = line * full;
+    best.width = (int)w, best.tpr = tpr;
+  }
+  if (!best.width) return best;
+  best.threads = 256;
+  while (best.threads < 1024 && pixels > 2 * (best.threads / best.tpr)) best.threads *= 2;
+  const int64_t r = up(pixels, best.threads / best.tpr);
+  best.r = r <= 1 ? 1 : r <= 2 ? 2 : r <= 4 ? 4 : 8;
+  // few large blocks leave most of the CUs idle for longer than two more launches take
+  if (batch * up(cols, best.width) < 128 && best.threads * best.r > 1024) best.width = 0;
+  return best;
+}
+
+size_t part_bytes(int64_t batch, int64_t cols) {
+  return a256((size_t)most_units(batch, cols) * (size_t)cols * 8);
+}
+size_t need_bytes(int64_t batch, int64_t cols, int64_t groups) {
+  return part_bytes(batch, cols) + a256((size_t)batch * (size_t)groups * 8);
 }
 
 int gn_shape(int64_t batch, int64_t pixels, int64_t channels, int64_t groups, int32_t dtype) {
@@ -484,20 +780,42 @@ int gn_shape(int64_t batch, int64_t pixels, int64_t channels, int64_t groups, in
 }
 
 int gn_args(int64_t batch, int64_t pixels, int64_t channels, int64_t groups, void *ws,
-            size_t ws_bytes, GnArgs *a, Split *s) {
+            size_t ws_bytes, GnArgs *a) {
   if (!ws || ((uintptr_t)ws & 15)) return refuse(LRCNN_EINVAL, "workspace null or misaligned");
-  *s = split_of(batch, pixels, channels);
-  const size_t need = need_bytes(*s, batch, channels, groups);
+  const size_t need = need_bytes(batch, channels, groups);
   if (ws_bytes < need)
     return refuse(LRCNN_EWORKSPACE, "workspace needs ", need, " bytes, got ", ws_bytes);
-  a->pixels = pixels, a->slab = s->slab, a->slabs = (int)s->slabs, a->batch = (int)batch;
-  a->units = batch * s->slabs;
+  a->pixels = pixels, a->batch = (int)batch;
   a->cols = (int)channels, a->pitch = (int)pitch_of(channels);
   a->groups = (int)groups, a->per = (int)(channels / groups);
-  a->tpr = s->tpr, a->ctiles = s->ctiles;
+  a->by_per = fast_div((uint32_t)a->per);
+  a->inv = 1.0 / ((double)pixels * (double)a->per);
   a->part = (float2 *)ws;
-  a->stat = (float2 *)((char *)ws + part_bytes(*s, channels));
+  a->stat = (float2 *)((char *)ws + part_bytes(batch, channels));
   return LRCNN_OK;
+}
+// The passes over slabs
+void cut(GnArgs *a) {
+  const Split s = split_of(a->batch, a->pixels, a->cols);
+  a->slab = s.slab, a->slabs = (int)s.slabs, a->units = a->batch * s.slabs;
+  a->tpr = s.tpr, a->ctiles = s.ctiles;
+}
+
+unsigned blocks_of(GnArgs *a, const Block &b) {
+  a->width = b.width, a->tpr = b.tpr;
+  a->ctiles = (int)up(a->cols, b.width);
+  return (unsigned)((int64_t)a->batch * a->ctiles);
+}
+size_t lds_of(const Block &b) {
+  return (size_t)b.tpr * kVec * (8 + b.threads / 64 * 2 * 4 + 4);
+}
+template <int MOST, typename F>
+void by_r(int r, F &&f) {
+  using std::integral_constant;
+  if (r == 1) f(integral_constant<int, 1>());
+  else if (r == 2) f(integral_constant<int, 2>());
+  else if (r == 4 || MOST == 4) f(integral_constant<int, 4>());
+  else f(integral_constant<int, MOST>());
 }
 
 }  // namespace
@@ -515,7 +833,7 @@ extern "C" int lrcnn_group_norm_workspace_bytes(int64_t batch, int64_t pixels, i
                                                 int64_t groups, size_t *bytes) {
   if (!bytes) return refuse(LRCNN_EINVAL, "null output");
   TRY(gn_shape(batch, pixels, channels, groups, LRCNN_F32));
-  *bytes = need_bytes(split_of(batch, pixels, channels), batch, channels, groups);
+  *bytes = need_bytes(batch, channels, groups);
   return LRCNN_OK;
 }
 
@@ -540,18 +858,28 @@ extern "C" int lrcnn_group_norm_forward(int64_t batch, int64_t pixels, int64_t c
   TRY(take_f32("mean", mean, false));
   TRY(take_f32("rstd", rstd, false));
   TRY(take_ckpt("ckpt", ckpt, false));
-  Split sp;
-  TRY(gn_args(batch, pixels, channels, groups, workspace, ws_bytes, &a, &sp));
+  TRY(gn_args(batch, pixels, channels, groups, workspace, ws_bytes, &a));
   a.eps = eps, a.gamma = gamma, a.beta = beta, a.mean_out = mean, a.rstd_out = rstd;
   a.k = ckpt_of(ckpt, batch * pixels, channels);
   hipStream_t s = (hipStream_t)stream;
-  const unsigned grid = (unsigned)(a.units * a.ctiles);
+  const Block one = block_of(batch, pixels, channels, a.per, es, ckpt != nullptr, es == 2 ? 8 : 4);
   return by_kind_or_none(kind, [&](auto K) {
     auto run = [&](auto *t) {
       using T = std::remove_pointer_t<decltype(t)>;
-      gn_stats_kernel<T><<<grid, 256, 0, s>>>(a);
-      gn_group_kernel<<<(unsigned)(batch * groups), 256, 0, s>>>(a);
-      gn_apply_kernel<T, K.value><<<grid, 256, 0, s>>>(a);
+      if (one.width) {
+        GnArgs w = a;
+        const unsigned g = blocks_of(&w, one);
+        by_r<sizeof(T) == 2 ? 8 : 4>(one.r, [&](auto r) {
+          gn_whole_kernel<T, K.value, r.value><<<g, one.threads, lds_of(one), s>>>(w);
+        });
+        return;
+      }
+      GnArgs w = a;
+      cut(&w);
+      const unsigned grid = (unsigned)(w.units * w.ctiles);
+      gn_stats_kernel<T><<<grid, 256, 0, s>>>(w);
+      gn_group_kernel<<<(unsigned)(batch * groups), 1024, 0, s>>>(w);
+      gn_apply_kernel<T, K.value><<<grid, 256, 0, s>>>(w);
     };
     if (dtype == LRCNN_BF16) run((bf16 *)nullptr);
     else run((float *)nullptr);
@@ -589,25 +917,38 @@ extern "C" int lrcnn_group_norm_backward(int64_t batch, int64_t pixels, int64_t 
   }
   const bool grads = dgamma || dbeta;
   if (!some && (!grads || accumulate)) return LRCNN_OK;
-  Split sp;
-  TRY(gn_args(batch, pixels, channels, groups, workspace, ws_bytes, &a, &sp));
+  TRY(gn_args(batch, pixels, channels, groups, workspace, ws_bytes, &a));
   a.mean = mean, a.rstd = rstd, a.gamma = gamma, a.beta = beta;
   a.dgamma = dgamma, a.dbeta = dbeta, a.accumulate = accumulate != 0;
   a.k = ckpt_of(ckpt, batch * pixels, channels);
   hipStream_t s = (hipStream_t)stream;
-  if (!some) a.batch = 0, a.units = 0;
-  const unsigned join = (unsigned)(a.batch * (int64_t)groups + (grads ? up(channels, 32) : 0));
+  const unsigned chans = (unsigned)up(channels, 32);
   if (!some) {  // no rows: the gradients are zero
-    gn_join_kernel<<<join, 1024, 0, s>>>(a);
+    a.units = 0;
+    gn_grads_kernel<<<chans, 1024, 0, s>>>(a);
     return launched("group_norm_backward");
   }
-  const unsigned grid = (unsigned)(a.units * a.ctiles);
+  const Block one = block_of(batch, pixels, channels, a.per, es, ckpt != nullptr, 4);
   return by_kind_or_none(kind, [&](auto K) {
     auto run = [&](auto *t, auto ck) {
       using T = std::remove_pointer_t<decltype(t)>;
-      gn_sums_kernel<T, K.value, ck.value><<<grid, 256, 0, s>>>(a);
-      gn_join_kernel<<<join, 1024, 0, s>>>(a);
-      gn_dx_kernel<T, K.value, ck.value><<<grid, 256, 0, s>>>(a);
+      if (one.width) {
+        GnArgs w = a;
+        const unsigned g = blocks_of(&w, one);
+        if (!grads) w.part = nullptr;
+        by_r<4>(one.r, [&](auto r) {
+          gn_whole_back_kernel<T, K.value, ck.value, r.value><<<g, one.threads, lds_of(one), s>>>(w);
+        });
+        w.units = batch;
+        if (grads && batch > 1) gn_grads_kernel<<<chans, 1024, 0, s>>>(w);
+        return;
+      }
+      GnArgs w = a;
+      cut(&w);
+      const unsigned grid = (unsigned)(w.units * w.ctiles);
+      gn_sums_kernel<T, K.value, ck.value><<<grid, 256, 0, s>>>(w);
+      gn_join_kernel<<<(unsigned)(batch * groups) + (grads ? chans : 0), 1024, 0, s>>>(w);
+      gn_dx_kernel<T, K.value, ck.value><<<grid, 256, 0, s>>>(w);
     };
     auto typed = [&](auto *t) {
       if (ckpt) run(t, std::true_type());

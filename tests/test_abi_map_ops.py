@@ -172,7 +172,7 @@ def z(*s, **k):
 
 
 def test_binding_refuses_tensors_that_do_not_agree():
-    ws, ck = z(1 << 16, dtype=torch.uint8), z(1 << 14, dtype=torch.uint8)
+    ws, ck = z(1 << 20, dtype=torch.uint8), z(1 << 14, dtype=torch.uint8)
     x, c, rng = z(6, 40), z(40), z(2, dtype=torch.int64)
 
     def refused(code, fn, *a, **k):
@@ -247,7 +247,7 @@ def test_binding_refuses_host_tensors(name, stream, monkeypatch):
     monkeypatch.setattr(L.LIB, name, lambda *a: reached.append(a) or 0)
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 0, raising=False)
     with pytest.raises(L.LrcnnError) as e:
-        CALLS[name](z(1 << 16, dtype=torch.uint8), **stream)
+        CALLS[name](z(1 << 20, dtype=torch.uint8), **stream)
     assert e.value.code == EINVAL and "GPU" in str(e.value)
     assert not reached
 
@@ -261,7 +261,7 @@ def test_binding_refuses_tensors_of_another_gpu(stream, monkeypatch):
     monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 1)
     for name, call in CALLS.items():
         monkeypatch.setattr(L.LIB, name, lambda *a: calls.append(a[-1]) or 0)
-        run = lambda: call(z(1 << 16, dtype=torch.uint8), stream=stream)
+        run = lambda: call(z(1 << 20, dtype=torch.uint8), stream=stream)
         monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
         with pytest.raises(L.LrcnnError) as e:
             run()
