@@ -20,6 +20,7 @@ namespace act8 {
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int64_t kMaxFeatures = 1 << 24, kMaxFfnRows = 1 << 30;
 constexpr int kRow = 128;  // bytes of a tile's row in LDS: 64 bfloat16 or 32 float32 of depth
@@ -53,6 +54,7 @@ __device__ __forceinline__ void each(F &&f) {
 }
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+constexpr int least(int a, int b) { return a < b ? a : b; }
 // The wave's LDS accesses before are done as its other lanes see them
 __device__ __forceinline__ void wave_meets() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -364,26 +366,29 @@ __global__ __launch_bounds__(TL::THREADS) void ffn_kernel(FfnArgs a) {
       st = st == ST - 1 ? 0 : st + 1;
     }
   } else {
+    typedef std::conditional_t<sizeof(T) == 2, u32x4_a2, u32x4_a4> u32x4_a;
     u32x4 reg[NF + NR];
     auto fetch = [&]() {
-      const int n = a.depth - kpos;
+      if (kpos - vec * E + BK <= a.depth) {  // (the same for all threads)
 #pragma unroll
-      for (int j = 0; j < NF + NR; ++j) {
-        if constexpr (sizeof(T) == 2) {
-          reg[j] = __builtin_bit_cast(u32x4, load8((const bf16 *)gp[j], n).w);
-        } else {
-          const float *p = (const float *)gp[j];
-          f32x4 v;
-          if (n >= 4) {
-            v = __builtin_bit_cast(f32x4, *(const f32x4_a4 *)p);
-          } else {
+        for (int j = 0; j < NF + NR; ++j) reg[j] = *(const u32x4_a *)gp[j];
+      } else {
+        const int n = a.depth - kpos;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = e < n ? p[e] : 0.f;
-          }
-          reg[j] = __builtin_bit_cast(u32x4, v);
+        for (int j = 0; j < NF + NR; ++j) {
+          const T *p = (const T *)gp[j];
+          uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (e < n) {
+              if constexpr (sizeof(T) == 2) w[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
+              else w[e] = __float_as_uint(p[e]);
+            }
+          reg[j] = (u32x4){w[0], w[1], w[2], w[3]};
         }
-        gp[j] += kRow;
       }
+#pragma unroll
+      for (int j = 0; j < NF + NR; ++j) gp[j] += kRow;
       kpos += BK;
     };
     auto keep = [&](int st) {
@@ -447,11 +452,12 @@ __global__ __launch_bounds__(TL::THREADS) void ffn_kernel(FfnArgs a) {
   }
 }
 
-// Large products: 256 features by 256 rows, four waves of 128 x 128, one on each matrix
-// pipe. A wave reads (128 + 128) rows of fragments for 128 x 128 products; with
-// half-sized ones, eight to a tile, the LDS reads and the copies into it would take as
-// long as the products. Tile rows of 128 bytes (64 bfloat16 or 32 float32 of depth):
-// whole cache lines; with rows of 64 bytes and twice the stages the L2's requests bound it.
+// Large products: four waves of FB x RB blocks of 32 x 32, one on each matrix pipe, two by
+// two. Of 128 x 128 (FB = RB = 4) a wave reads (128 + 128) rows of fragments for 128 x 128
+// products; with half-sized ones, eight waves to a tile, the LDS reads and the copies into it
+// would take as long as the products. Tile rows of 128 bytes (64 bfloat16 or 32
+// float32 of depth): whole cache lines; with rows of 64 bytes and twice the stages the
+// L2's requests bound it. Two stages, of 64 KB with FB = RB = 4.
 //
 // A step has four slices of 16 bytes. Its order is laid down slot by slot, one block's
 // products to a slot: each slice reads the next one's fragments; before the last one
@@ -459,7 +465,6 @@ __global__ __launch_bounds__(TL::THREADS) void ffn_kernel(FfnArgs a) {
 // during it the other stage's first fragments are read and this stage is copied over with
 // the step two ahead, which has the next step's first three slices to arrive. Past
 // the last step zeros are copied, so every step is alike.
-constexpr int kBigTile = 256, kBackPart = 40960;
 // Four neighbouring exponent bytes, of those that there are
 __device__ __forceinline__ uint32_t exponents4(const Ckpt &k, int64_t row, int c) {
   typedef uint32_t u32_a1 __attribute__((aligned(1)));
@@ -472,23 +477,32 @@ __device__ __forceinline__ uint32_t exponents4(const Ckpt &k, int64_t row, int c
     if (i * kGroup < left) e |= (uint32_t)p[i] << (8 * i);
   return e;
 }
-template <typename T, int EPI>
-__global__ __launch_bounds__(256, 1) void ffn_big_kernel(FfnArgs a) {
+template <int FB_, int RB_>
+struct Wide {
+  static constexpr int FB = FB_, RB = RB_, F = 64 * FB, R = 64 * RB, STAGE = (F + R) * kRow;
+  // EPI_BACK, 128 features a wave: a strip of 64 features and the codes of u and v
+  static constexpr int PART = 8192 + 8192 * RB;
+  static constexpr int LDS = FB == 4 && 4 * PART > 2 * STAGE ? 4 * PART : 2 * STAGE;
+};
+template <typename T, typename W, int EPI>
+__global__ __launch_bounds__(256, W::FB * W::RB > 4 ? 1 : 2) void ffn_wide_kernel(FfnArgs a) {
   constexpr int E = 16 / (int)sizeof(T), BK = kRow / (int)sizeof(T);
-  constexpr int STAGE = 2 * kBigTile * kRow, LD = 16;
-  __shared__ __align__(16) char smem[EPI == EPI_BACK ? 4 * kBackPart : 2 * STAGE];
+  constexpr int FB = W::FB, RB = W::RB, STAGE = W::STAGE;
+  constexpr int LF = W::F / 32, LD = LF + W::R / 32;  // copies a thread and step
+  constexpr bool CODES = EPI == EPI_BACK && FB == 4;
+  __shared__ __align__(16) char smem[CODES ? W::LDS : 2 * STAGE];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int tx, ty;
   tile_of(a, &tx, &ty);
-  const int r0 = tx * kBigTile, f0 = ty * (EPI == EPI_GATE ? kBigTile / 2 : kBigTile);
+  const int r0 = tx * W::R, f0 = ty * (EPI == EPI_GATE ? W::F / 2 : W::F);
   const int steps = (a.depth + BK - 1) / BK;
   // rows tid / 8 + 32 j of each operand, one vector each, to slot tid % 8
   const int br = tid >> 3, vec = (tid & 7) ^ ((tid >> 4) & 7);
   uint32_t off[LD];
   const int first = min(r0, a.rows - 1);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
+  for (int j = 0; j < LF; ++j) {
     const int t = br + 32 * j;
     int64_t f;
     if constexpr (EPI == EPI_GATE) {
@@ -498,8 +512,12 @@ __global__ __launch_bounds__(256, 1) void ffn_big_kernel(FfnArgs a) {
       f = min(f0 + t, a.feats - 1);
     }
     off[j] = (uint32_t)((f * a.depth + vec * E) * (int64_t)sizeof(T));
-    off[8 + j] = (uint32_t)(((int64_t)(min(r0 + t, a.rows - 1) - first) * a.x.ld + vec * E) *
-                            (int64_t)sizeof(T));
+  }
+#pragma unroll
+  for (int j = LF; j < LD; ++j) {
+    const int t = br + 32 * (j - LF);
+    off[j] = (uint32_t)(((int64_t)(min(r0 + t, a.rows - 1) - first) * a.x.ld + vec * E) *
+                        (int64_t)sizeof(T));
   }
   const char *gw = a.w, *gx = a.x.p + (int64_t)first * a.x.ld * (int64_t)sizeof(T);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem +
@@ -509,21 +527,21 @@ __global__ __launch_bounds__(256, 1) void ffn_big_kernel(FfnArgs a) {
   auto bring = [&](int st, int j, auto whole) {
     const uint32_t to = lds0 + st * STAGE + 32 * kRow * j;
     if constexpr (decltype(whole)::value) {
-      copy16(j < 8 ? gw : gx, off[j], to);
+      copy16(j < LF ? gw : gx, off[j], to);
     } else {
       const bool ok = kpos + vec * E < a.depth;
-      copy16(ok ? (j < 8 ? gw : gx) + off[j] : (const char *)&g_zero16[0], to);
+      copy16(ok ? (j < LF ? gw : gx) + off[j] : (const char *)&g_zero16[0], to);
     }
   };
   auto advance = [&]() {
     kpos += BK, gw += kRow, gx += kRow;
     asm volatile("" : "+s"(gw), "+s"(gx));
   };
-  f32x16 acc[4][4];
+  f32x16 acc[FB][RB];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < FB; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < RB; ++j)
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
   const int wf = wave & 1, wr = wave >> 1;
@@ -534,24 +552,25 @@ __global__ __launch_bounds__(256, 1) void ffn_big_kernel(FfnArgs a) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const int r = lane & 31, at = r * kRow + swz<8>(r, 4 * (lane >> 5) + q) * 16;
-    pw[q] = at + wf * 128 * kRow;
-    px[q] = at + (kBigTile + wr * 128) * kRow;
+    pw[q] = at + wf * 32 * FB * kRow;
+    px[q] = at + (W::F + wr * 32 * RB) * kRow;
   }
-  u32x4 fw[2][4], fx[2][4];
+  u32x4 fw[2][FB], fx[2][RB];
   // fragment k of slice q: the first weights', the rows', then the other weights'
   auto fragment = [&](int st, auto q_, auto k_) {
     constexpr int q = decltype(q_)::value, k = decltype(k_)::value, p = q & 1;
     if constexpr (k == 0) fw[p][0] = *(lds_u32x4 *)(lds + st * STAGE + pw[q]);
-    else if constexpr (k < 5)
+    else if constexpr (k <= RB)
       fx[p][k - 1] = *(lds_u32x4 *)(lds + st * STAGE + px[q] + (k - 1) * 32 * kRow);
-    else fw[p][k - 4] = *(lds_u32x4 *)(lds + st * STAGE + pw[q] + (k - 4) * 32 * kRow);
+    else fw[p][k - RB] = *(lds_u32x4 *)(lds + st * STAGE + pw[q] + (k - RB) * 32 * kRow);
   };
   using std::integral_constant;
   // slice q of the step on stage st
   auto slice = [&](auto q_, int st, auto whole) {
     constexpr int q = decltype(q_)::value, p = q & 1;
-    each<0, 16>([&](auto m_) {
-      constexpr int m = decltype(m_)::value, i = m / 4, j = m % 4;
+    constexpr int S = FB * RB, N = FB + RB;  // slots, fragments
+    each<0, S>([&](auto m_) {
+      constexpr int m = decltype(m_)::value, i = m / RB, j = m % RB;
       if constexpr (sizeof(T) == 2) {
         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fw[p][i]),
                                                             __builtin_bit_cast(bf16x8, fx[p][j]),
@@ -563,8 +582,12 @@ __global__ __launch_bounds__(256, 1) void ffn_big_kernel(FfnArgs a) {
                                                            __uint_as_float(fx[p][j][e]),
                                                            acc[i][j], 0, 0, 0);
       }
-      if constexpr (m < 8) fragment(q == 3 ? st ^ 1 : st, integral_constant<int, (q + 1) % 4>(), m_);
-      if constexpr (q == 3) bring(st, m, whole);
+      constexpr int L = S > 8 ? S / 2 : S;  // the reads in the first L slots
+      each<N * least(m, L) / L, N * least(m + 1, L) / L>([&](auto k) {
+        fragment(q == 3 ? st ^ 1 : st, integral_constant<int, (q + 1) % 4>(), k);
+      });
+      if constexpr (q == 3)
+        each<LD * m / S, LD * (m + 1) / S>([&](auto j) { bring(st, j, whole); });
       __builtin_amdgcn_sched_barrier(0);
     });
   };
@@ -584,26 +607,28 @@ __global__ __launch_bounds__(256, 1) void ffn_big_kernel(FfnArgs a) {
   }
   wait_vmcnt<LD>();
   __syncthreads();
-  each<0, 8>([&](auto k) { fragment(0, integral_constant<int, 0>(), k); });
+  each<0, FB + RB>([&](auto k) { fragment(0, integral_constant<int, 0>(), k); });
   int t = 0;
   for (; kpos + BK <= a.depth; ++t) step(t & 1, std::true_type());
   for (; t < steps; ++t) step(t & 1, std::false_type());
   wait_vmcnt<0>();
-  const int wrow = r0 + wr * 128;
-  if constexpr (EPI != EPI_BACK) {
-    const int c0 = f0 + wf * Lanes<EPI, 4>::WIDTH;
+  const int wrow = r0 + wr * 32 * RB;
+  __syncthreads();
+  if constexpr (!CODES) {
+    const int c0 = f0 + wf * Lanes<EPI, FB>::WIDTH, k = lane % Lanes<EPI, FB>::PER;
     Bias bias;
-    bias.load<EPI>(a, c0 + 8 * (lane % Lanes<EPI, 4>::PER));
-    __syncthreads();
-    lds_char *const strip = (lds_char *)smem + wave * 32 * 128 * 4;
+    bias.load<EPI>(a, c0 + 8 * k);
+    lds_char *const strip = (lds_char *)smem + wave * 32 * 32 * FB * 4;
 #pragma unroll 1
-    for (int j = 0; j < 4; ++j) {
-      each<0, 4>([&](auto j_) {
-        if (j == j_) each<0, 4>([&](auto i) { strip_put<4>(strip, i, acc[i][j_]); });
+    for (int j = 0; j < RB; ++j) {
+      each<0, RB>([&](auto j_) {
+        if (j == j_) each<0, FB>([&](auto i) { strip_put<FB>(strip, i, acc[i][j_]); });
       });
       wave_meets();
-      strip_rows<T, EPI, 4>(a, strip, wrow + 32 * j, c0, bias,
-                            [](int, float (&)[8], float (&)[8]) {});
+      const int rj = wrow + 32 * j;
+      strip_rows<T, EPI, FB>(a, strip, rj, c0, bias, [&](int row, float (&u)[8], float (&v)[8]) {
+        read_uv<T>(a, rj + row, c0 + 8 * k, u, v);
+      });
       wave_meets();
     }
   } else {
@@ -611,13 +636,15 @@ __global__ __launch_bounds__(256, 1) void ffn_big_kernel(FfnArgs a) {
     // each for 32 rows of 128 features. They are all on their way before the first
     // store, as a wait for a load waits for the stores before it.
     const int c0 = f0 + wf * 128;
-    lds_char *const strip = (lds_char *)smem + wave * kBackPart, *const held = strip + 8192;
-    __syncthreads();
+    lds_char *const strip = (lds_char *)smem + wave * W::PART, *const held = strip + 8192;
     const bool ck = a.ku.q != nullptr;
-    uint32_t eu[2] = {0, 0}, ev[2] = {0, 0};  // exponents of rows lane and lane + 64
+    constexpr int HR = (RB + 1) / 2;
+    uint32_t eu[HR], ev[HR];  // exponents of rows lane and lane + 64
+#pragma unroll
+    for (int h = 0; h < HR; ++h) eu[h] = ev[h] = 0;
     if (ck && c0 < a.feats) {
 #pragma unroll 4
-      for (int i = 0; i < 16; ++i) {
+      for (int i = 0; i < 4 * RB; ++i) {
         const int row = 8 * i + lane / 8, c = c0 + ((lane & 7) ^ (row & 7)) * 16;
         const int64_t r = min(wrow + row, a.rows - 1);
         const bool ok = c < a.ku.pitch;
@@ -627,7 +654,7 @@ __global__ __launch_bounds__(256, 1) void ffn_big_kernel(FfnArgs a) {
         copy16(ok ? (const char *)a.kv.q + r * a.kv.pitch + c : zero, to + 4096);
       }
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < HR; ++h) {
         const int64_t r = min(wrow + 64 * h + lane, a.rows - 1);
         eu[h] = exponents4(a.ku, r, c0);
         ev[h] = exponents4(a.kv, r, c0);
@@ -635,15 +662,15 @@ __global__ __launch_bounds__(256, 1) void ffn_big_kernel(FfnArgs a) {
       wait_vmcnt<0>();
     }
 #pragma unroll 1
-    for (int jh = 0; jh < 8; ++jh) {
-      each<0, 8>([&](auto x) {
+    for (int jh = 0; jh < 2 * RB; ++jh) {
+      each<0, 2 * RB>([&](auto x) {
         constexpr int j = decltype(x)::value / 2, h = decltype(x)::value % 2;
         if (jh == x)
           each<0, 2>([&](auto i) { strip_put<2>(strip, i, acc[2 * h + i][j]); });
       });
       wave_meets();
       const int j = jh >> 1, h = jh & 1, rj = wrow + 32 * j;
-      const uint32_t wu = j < 2 ? eu[0] : eu[1], wv = j < 2 ? ev[0] : ev[1];
+      const uint32_t wu = j < 2 ? eu[0] : eu[HR - 1], wv = j < 2 ? ev[0] : ev[HR - 1];
       strip_rows<T, EPI, 2>(
           a, strip, rj, c0 + 64 * h, Bias(), [&](int row, float (&u)[8], float (&v)[8]) {
             const int k = lane & 7;
@@ -771,8 +798,13 @@ __global__ __launch_bounds__(512) void ffn_few_kernel(FfnArgs a) {
 }
 
 // ------------------------------------------------------------- launches
-typedef Tile<2, 2, 2, 2, 1, 2> Mid;    // 128 x 128, 4 waves
+typedef Wide<4, 4> Big;                // 256 features x 256 rows
+typedef Wide<4, 2> Half;               // 256 x 128
+typedef Wide<2, 2> Mid;                // 128 x 128
+typedef Tile<2, 2, 2, 2, 1, 2> Plain;  // 128 x 128 of operands that are not aligned
 typedef Tile<1, 2, 1, 2, 4, 3> Small;  // 64 x 64, 4 waves that split the depth
+typedef Tile<1, 2, 1, 1, 4, 3> Tiny;   // 64 x 32
+typedef Tile<1, 1, 1, 1, 4, 3> Least;  // 32 x 32, one block of features
 constexpr int kFewRows = 32;
 
 int lay_out(FfnArgs &a, int rows, int feats) {
@@ -788,6 +820,14 @@ int launch(FfnArgs &a, hipStream_t s) {
   const int st = lay_out(a, TL::R, EPI == EPI_GATE ? TL::F / 2 : TL::F);
   if (st != LRCNN_OK) return st;
   ffn_kernel<T, TL, EPI, DMA><<<(unsigned)(a.gx * a.gy), TL::THREADS, 0, s>>>(a);
+  return LRCNN_OK;
+}
+
+template <typename T, typename W, int EPI>
+int launch_wide(FfnArgs &a, hipStream_t s) {
+  const int st = lay_out(a, W::R, EPI == EPI_GATE ? W::F / 2 : W::F);
+  if (st != LRCNN_OK) return st;
+  ffn_wide_kernel<T, W, EPI><<<(unsigned)(a.gx * a.gy), 256, 0, s>>>(a);
   return LRCNN_OK;
 }
 
@@ -808,17 +848,14 @@ int product(FfnArgs a, hipStream_t s) {
   auto tiles = [&](int64_t f, int64_t r) {
     return (((int64_t)a.feats * H + f - 1) / f) * ((a.rows + r - 1) / r);
   };
+  // (the wide tiles' copies have 32-bit offsets)
+  const bool near = (int64_t)a.feats * H * a.depth * (int64_t)sizeof(T) < (int64_t)1 << 32 &&
+                    Big::R * a.x.ld * (int64_t)sizeof(T) < (int64_t)1 << 32;
   if (tiles(Mid::F, Mid::R) < 256)
     return dma ? launch<T, Small, EPI, true>(a, s) : launch<T, Small, EPI, false>(a, s);
-  if (!dma) return launch<T, Mid, EPI, false>(a, s);
-  // (the large tile's copies have 32-bit offsets)
-  const bool near = (int64_t)a.feats * H * a.depth * (int64_t)sizeof(T) < (int64_t)1 << 32 &&
-                    kBigTile * a.x.ld * (int64_t)sizeof(T) < (int64_t)1 << 32;
-  if (!near || tiles(kBigTile, kBigTile) < 256) return launch<T, Mid, EPI, true>(a, s);
-  const int st = lay_out(a, kBigTile, kBigTile / H);
-  if (st != LRCNN_OK) return st;
-  ffn_big_kernel<T, EPI><<<(unsigned)(a.gx * a.gy), 256, 0, s>>>(a);
-  return LRCNN_OK;
+  if (!dma || !near) return launch<T, Plain, EPI, false>(a, s);
+  if (tiles(Big::F, Big::R) < 256) return launch_wide<T, Mid, EPI>(a, s);
+  return launch_wide<T, Big, EPI>(a, s);
 }
 
 template <int EPI>
