@@ -277,6 +277,17 @@ __device__ __forceinline__ void copy16(const char *base, uint32_t off, uint32_t 
                : "memory", "m0");
 }
 
+// Waits until at most min(k, MOST) steps' copies of LD each are on their way
+template <int LD, int MOST>
+__device__ __forceinline__ void wait_tiles(int k) {
+  if constexpr (MOST > 0) {
+    if (k >= MOST) return wait_vmcnt<MOST * LD>();
+    wait_tiles<LD, MOST - 1>(k);
+  } else {
+    wait_vmcnt<0>();
+  }
+}
+
 // DMA: rows of both operands at 16-byte steps from aligned bases and a depth of whole
 // 16-byte vectors: copied straight into LDS. Else through registers, at the elements'
 // alignment.
@@ -358,8 +369,7 @@ __global__ __launch_bounds__(TL::THREADS) void ffn_kernel(FfnArgs a) {
       if (i < steps) bring(i);
     int st = 0;
     for (int t = 0; t < steps; ++t) {
-      if (ST > 2 && t + 1 < steps) wait_vmcnt<(ST - 2) * LD>();
-      else wait_vmcnt<0>();
+      wait_tiles<LD, ST - 2>(steps - 1 - t);
       __syncthreads();
       if (t + ST - 1 < steps) bring(st == 0 ? ST - 1 : st - 1);
       multiply(st);
@@ -460,11 +470,14 @@ __global__ __launch_bounds__(TL::THREADS) void ffn_kernel(FfnArgs a) {
 // L2's requests bound it. Two stages, of 64 KB with FB = RB = 4.
 //
 // A step has four slices of 16 bytes. Its order is laid down slot by slot, one block's
-// products to a slot: each slice reads the next one's fragments; before the last one
-// the waves meet -- the other stage has arrived, this one has been read by all -- and
-// during it the other stage's first fragments are read and this stage is copied over with
-// the step two ahead, which has the next step's first three slices to arrive. Past
-// the last step zeros are copied, so every step is alike.
+// products to a slot, with a share of the LDS reads of later slices' fragments and of the
+// copies of a later step. A copy holds the memory pipe of the CU for 16 cycles, so the
+// 4 LD of a step are spread over several slices: in one they stall the products. After
+// the second slice all of the step's fragments are on their way or read, the waves meet,
+// and its stage may be copied over. With two stages the copies of the step two ahead go
+// out in three slices and have two to arrive, until the waves meet again before the
+// fourth. With more they go out in four, and once a step the waves meet. Past the last
+// step zeros are copied, so every step is alike.
 // Four neighbouring exponent bytes, of those that there are
 __device__ __forceinline__ uint32_t exponents4(const Ckpt &k, int64_t row, int c) {
   typedef uint32_t u32_a1 __attribute__((aligned(1)));
@@ -477,20 +490,21 @@ __device__ __forceinline__ uint32_t exponents4(const Ckpt &k, int64_t row, int c
     if (i * kGroup < left) e |= (uint32_t)p[i] << (8 * i);
   return e;
 }
-template <int FB_, int RB_>
+template <int FB_, int RB_, int ST_>
 struct Wide {
   static constexpr int FB = FB_, RB = RB_, F = 64 * FB, R = 64 * RB, STAGE = (F + R) * kRow;
+  static constexpr int ST = ST_;
   // EPI_BACK, 128 features a wave: a strip of 64 features and the codes of u and v
   static constexpr int PART = 8192 + 8192 * RB;
-  static constexpr int LDS = FB == 4 && 4 * PART > 2 * STAGE ? 4 * PART : 2 * STAGE;
+  static constexpr int LDS = FB == 4 && 4 * PART > ST * STAGE ? 4 * PART : ST * STAGE;
 };
 template <typename T, typename W, int EPI>
-__global__ __launch_bounds__(256, W::FB * W::RB > 4 ? 1 : 2) void ffn_wide_kernel(FfnArgs a) {
+__global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(FfnArgs a) {
   constexpr int E = 16 / (int)sizeof(T), BK = kRow / (int)sizeof(T);
-  constexpr int FB = W::FB, RB = W::RB, STAGE = W::STAGE;
+  constexpr int FB = W::FB, RB = W::RB, STAGE = W::STAGE, ST = W::ST;
   constexpr int LF = W::F / 32, LD = LF + W::R / 32;  // copies a thread and step
   constexpr bool CODES = EPI == EPI_BACK && FB == 4;
-  __shared__ __align__(16) char smem[CODES ? W::LDS : 2 * STAGE];
+  __shared__ __align__(16) char smem[CODES ? W::LDS : ST * STAGE];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int tx, ty;
@@ -555,62 +569,98 @@ __global__ __launch_bounds__(256, W::FB * W::RB > 4 ? 1 : 2) void ffn_wide_kerne
     pw[q] = at + wf * 32 * FB * kRow;
     px[q] = at + (W::F + wr * 32 * RB) * kRow;
   }
-  u32x4 fw[2][FB], fx[2][RB];
+  u32x4 fw[4][FB], fx[4][RB];  // by slice
+  constexpr int S = FB * RB, N = FB + RB;  // slots of a slice, its fragments
   // fragment k of slice q: the first weights', the rows', then the other weights'
   auto fragment = [&](int st, auto q_, auto k_) {
-    constexpr int q = decltype(q_)::value, k = decltype(k_)::value, p = q & 1;
-    if constexpr (k == 0) fw[p][0] = *(lds_u32x4 *)(lds + st * STAGE + pw[q]);
+    constexpr int q = decltype(q_)::value, k = decltype(k_)::value;
+    if constexpr (k == 0) fw[q][0] = *(lds_u32x4 *)(lds + st * STAGE + pw[q]);
     else if constexpr (k <= RB)
-      fx[p][k - 1] = *(lds_u32x4 *)(lds + st * STAGE + px[q] + (k - 1) * 32 * kRow);
-    else fw[p][k - RB] = *(lds_u32x4 *)(lds + st * STAGE + pw[q] + (k - RB) * 32 * kRow);
+      fx[q][k - 1] = *(lds_u32x4 *)(lds + st * STAGE + px[q] + (k - 1) * 32 * kRow);
+    else fw[q][k - RB] = *(lds_u32x4 *)(lds + st * STAGE + pw[q] + (k - RB) * 32 * kRow);
   };
   using std::integral_constant;
-  // slice q of the step on stage st
-  auto slice = [&](auto q_, int st, auto whole) {
-    constexpr int q = decltype(q_)::value, p = q & 1;
-    constexpr int S = FB * RB, N = FB + RB;  // slots, fragments
+  // Slice q: reads READS slices' fragments from slice `from` on out of stage sr; copies
+  // the copies C0 .. C1 of a step to stage sc
+  auto slice = [&](auto q_, auto from, auto reads, int sr, auto c0, auto c1, int sc, auto whole) {
+    constexpr int q = decltype(q_)::value, K = decltype(reads)::value * N;
+    constexpr int B = decltype(c0)::value, C = decltype(c1)::value - B;
+    constexpr int L = S > 8 ? 3 * S / 4 : S;  // the reads in the first L slots
     each<0, S>([&](auto m_) {
       constexpr int m = decltype(m_)::value, i = m / RB, j = m % RB;
       if constexpr (sizeof(T) == 2) {
-        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fw[p][i]),
-                                                            __builtin_bit_cast(bf16x8, fx[p][j]),
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fw[q][i]),
+                                                            __builtin_bit_cast(bf16x8, fx[q][j]),
                                                             acc[i][j], 0, 0, 0);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fw[p][i][e]),
-                                                           __uint_as_float(fx[p][j][e]),
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fw[q][i][e]),
+                                                           __uint_as_float(fx[q][j][e]),
                                                            acc[i][j], 0, 0, 0);
       }
-      constexpr int L = S > 8 ? S / 2 : S;  // the reads in the first L slots
-      each<N * least(m, L) / L, N * least(m + 1, L) / L>([&](auto k) {
-        fragment(q == 3 ? st ^ 1 : st, integral_constant<int, (q + 1) % 4>(), k);
+      each<K * least(m, L) / L, K * least(m + 1, L) / L>([&](auto k) {
+        constexpr int x = decltype(k)::value;
+        fragment(sr, integral_constant<int, (decltype(from)::value + x / N) % 4>(),
+                 integral_constant<int, x % N>());
       });
-      if constexpr (q == 3)
-        each<LD * m / S, LD * (m + 1) / S>([&](auto j) { bring(st, j, whole); });
+      each<B + C * m / S, B + C * (m + 1) / S>([&](auto j) { bring(sc, j, whole); });
       __builtin_amdgcn_sched_barrier(0);
     });
   };
-  auto step = [&](int st, auto whole) {
-    slice(integral_constant<int, 0>(), st, whole);
-    slice(integral_constant<int, 1>(), st, whole);
-    slice(integral_constant<int, 2>(), st, whole);
-    wait_vmcnt<0>();
-    __syncthreads();
-    slice(integral_constant<int, 3>(), st, whole);
-    advance();
+#define I(x) integral_constant<int, (x)>()
+  // From a step's third slice to the next one's second. LAST: there is no next one.
+  int st = 0;
+  auto turn = [&](auto whole, auto last) {
+    constexpr bool LAST = decltype(last)::value;
+    const int nx = st == ST - 1 ? 0 : st + 1;
+    if constexpr (ST == 2) {
+      constexpr int C = LAST ? 0 : LD, C2 = 3 * C / 8, C3 = (C - C2) / 2 + C2;
+      __syncthreads();
+      slice(I(2), I(0), I(0), nx, I(0), I(C2), st, whole);
+      wait_vmcnt<C2>();
+      __syncthreads();
+      slice(I(3), I(0), I(LAST ? 0 : 1), nx, I(C2), I(C3), st, whole);
+      if constexpr (!LAST) {
+        slice(I(0), I(1), I(2), nx, I(C3), I(C), st, whole);
+        slice(I(1), I(3), I(1), nx, I(0), I(0), st, whole);
+      }
+    } else {
+      constexpr int C = LAST ? 0 : LD, R1 = LAST ? 0 : 1;
+      wait_vmcnt<(ST - 2) * LD>();
+      __syncthreads();
+      slice(I(2), I(0), I(R1), nx, I(0), I(C / 4), st, whole);
+      slice(I(3), I(1), I(R1), nx, I(C / 4), I(C / 2), st, whole);
+      if constexpr (!LAST) {
+        slice(I(0), I(2), I(1), nx, I(C / 2), I(3 * C / 4), st, whole);
+        slice(I(1), I(3), I(1), nx, I(3 * C / 4), I(C), st, whole);
+      }
+    }
+    if constexpr (!LAST) advance();
+    st = nx;
   };
-  for (int i = 0; i < 2; ++i) {
+  using std::false_type;
+  for (int i = 0; i < ST; ++i) {
 #pragma unroll
-    for (int j = 0; j < LD; ++j) bring(i, j, std::false_type());
+    for (int j = 0; j < LD; ++j) bring(i, j, false_type());
     advance();
   }
-  wait_vmcnt<LD>();
+  wait_vmcnt<(ST - 1) * LD>();
   __syncthreads();
-  each<0, FB + RB>([&](auto k) { fragment(0, integral_constant<int, 0>(), k); });
+  each<0, N>([&](auto k) { fragment(0, I(0), k); });
+  if constexpr (ST == 2) {
+    slice(I(0), I(1), I(2), 0, I(0), I(0), 0, false_type());
+    slice(I(1), I(3), I(1), 0, I(0), I(0), 0, false_type());
+  } else {
+    each<0, N>([&](auto k) { fragment(0, I(1), k); });
+    slice(I(0), I(2), I(1), 0, I(0), I(0), 0, false_type());
+    slice(I(1), I(3), I(1), 0, I(0), I(0), 0, false_type());
+  }
   int t = 0;
-  for (; kpos + BK <= a.depth; ++t) step(t & 1, std::true_type());
-  for (; t < steps; ++t) step(t & 1, std::false_type());
+  for (; kpos + BK <= a.depth; ++t) turn(std::true_type(), false_type());
+  for (; t + 1 < steps; ++t) turn(false_type(), false_type());
+  turn(false_type(), std::true_type());
+#undef I
   wait_vmcnt<0>();
   const int wrow = r0 + wr * 32 * RB;
   __syncthreads();
@@ -798,13 +848,14 @@ __global__ __launch_bounds__(512) void ffn_few_kernel(FfnArgs a) {
 }
 
 // ------------------------------------------------------------- launches
-typedef Wide<4, 4> Big;                // 256 features x 256 rows
-typedef Wide<4, 2> Half;               // 256 x 128
-typedef Wide<2, 2> Mid;                // 128 x 128
+typedef Wide<4, 4, 2> Big;                // 256 features x 256 rows
+typedef Wide<4, 2, 3> Half;               // 256 x 128
+typedef Wide<2, 2, 2> Mid;                // 128 x 128
+typedef Wide<2, 2, 4> Deep;            // 128 x 128, one workgroup a CU
 typedef Tile<2, 2, 2, 2, 1, 2> Plain;  // 128 x 128 of operands that are not aligned
-typedef Tile<1, 2, 1, 2, 4, 3> Small;  // 64 x 64, 4 waves that split the depth
-typedef Tile<1, 2, 1, 1, 4, 3> Tiny;   // 64 x 32
-typedef Tile<1, 1, 1, 1, 4, 3> Least;  // 32 x 32, one block of features
+typedef Tile<1, 2, 1, 2, 4, 5> Small;  // 64 x 64, 4 waves that split the depth
+typedef Tile<1, 2, 1, 1, 4, 5> Tiny;   // 64 x 32
+typedef Tile<1, 1, 1, 1, 4, 6> Least;  // 32 x 32, one block of features
 constexpr int kFewRows = 32;
 
 int lay_out(FfnArgs &a, int rows, int feats) {
