@@ -377,8 +377,9 @@ __global__ __launch_bounds__(TL::THREADS) void ffn_kernel(FfnArgs a) {
     }
   } else {
     typedef std::conditional_t<sizeof(T) == 2, u32x4_a2, u32x4_a4> u32x4_a;
-    u32x4 reg[NF + NR];
-    auto fetch = [&]() {
+    // (two steps' loads are on their way while a third is multiplied)
+    u32x4 reg0[NF + NR], reg1[NF + NR];
+    auto fetch = [&](u32x4 (&reg)[NF + NR]) {
       if (kpos - vec * E + BK <= a.depth) {  // (the same for all threads)
 #pragma unroll
         for (int j = 0; j < NF + NR; ++j) reg[j] = *(const u32x4_a *)gp[j];
@@ -401,21 +402,26 @@ __global__ __launch_bounds__(TL::THREADS) void ffn_kernel(FfnArgs a) {
       for (int j = 0; j < NF + NR; ++j) gp[j] += kRow;
       kpos += BK;
     };
-    auto keep = [&](int st) {
+    auto keep = [&](const u32x4 (&reg)[NF + NR], int st) {
 #pragma unroll
       for (int j = 0; j < NF + NR; ++j) {
         const int row = br + (j < NF ? RP * j : TL::F + RP * (j - NF));
         *(u32x4 *)(smem + st * TL::STAGE + row * kRow + (tid & 7) * 16) = reg[j];
       }
     };
-    fetch();
-    keep(0);
-    if (steps > 1) fetch();
-    for (int t = 0; t < steps; ++t) {
+    fetch(reg0);
+    keep(reg0, 0);
+    if (steps > 1) fetch(reg1);
+    if (steps > 2) fetch(reg0);
+    auto step = [&](int t, u32x4 (&next)[NF + NR]) {
       __syncthreads();
-      if (t + 1 < steps) keep((t + 1) & 1);
-      if (t + 2 < steps) fetch();
+      if (t + 1 < steps) keep(next, (t + 1) & 1);
+      if (t + 3 < steps) fetch(next);
       multiply(t & 1);
+    };
+    for (int t = 0; t < steps; t += 2) {
+      step(t, reg1);
+      if (t + 1 < steps) step(t + 1, reg0);
     }
   }
   const int c0 = f0 + wf * Lanes<EPI, FB>::WIDTH;
@@ -853,9 +859,9 @@ typedef Wide<4, 2, 3> Half;               // 256 x 128
 typedef Wide<2, 2, 2> Mid;                // 128 x 128
 typedef Wide<2, 2, 4> Deep;            // 128 x 128, one workgroup a CU
 typedef Tile<2, 2, 2, 2, 1, 2> Plain;  // 128 x 128 of operands that are not aligned
-typedef Tile<1, 2, 1, 2, 4, 5> Small;  // 64 x 64, 4 waves that split the depth
-typedef Tile<1, 2, 1, 1, 4, 5> Tiny;   // 64 x 32
-typedef Tile<1, 1, 1, 1, 4, 6> Least;  // 32 x 32, one block of features
+typedef Tile<1, 2, 1, 2, 4, 3> Small;  // 64 x 64, 4 waves that split the depth
+typedef Tile<1, 2, 1, 1, 4, 3> Tiny;   // 64 x 32
+typedef Tile<1, 1, 1, 1, 4, 3> Least;  // 32 x 32, one block of features
 constexpr int kFewRows = 32;
 
 int lay_out(FfnArgs &a, int rows, int feats) {
@@ -902,11 +908,52 @@ int product(FfnArgs a, hipStream_t s) {
   // (the wide tiles' copies have 32-bit offsets)
   const bool near = (int64_t)a.feats * H * a.depth * (int64_t)sizeof(T) < (int64_t)1 << 32 &&
                     Big::R * a.x.ld * (int64_t)sizeof(T) < (int64_t)1 << 32;
-  if (tiles(Mid::F, Mid::R) < 256)
-    return dma ? launch<T, Small, EPI, true>(a, s) : launch<T, Small, EPI, false>(a, s);
-  if (!dma || !near) return launch<T, Plain, EPI, false>(a, s);
-  if (tiles(Big::F, Big::R) < 256) return launch_wide<T, Mid, EPI>(a, s);
-  return launch_wide<T, Big, EPI>(a, s);
+  // The variant of the least estimated time: for n tiles on the busiest of 256 CUs,
+  // steps * max(alone, n * busy) + n * finish, in ns measured with one tile on a CU, with
+  // many, and for the results.
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int G = EPI == EPI_GATE ? 0 : EPI == EPI_BACK ? 1 : 2;
+  struct Cost {
+    int f, r, alone, busy, finish[3];
+    bool wide, plain;
+  };
+  constexpr Cost costs[] = {
+      {Big::F, Big::R, F32 ? 7100 : 1100, F32 ? 7100 : 1150, {20000, 40000, 6000}, true, false},
+      {Half::F, Half::R, F32 ? 3600 : 800, F32 ? 3600 : 900, {9000, 18000, 3000}, true, false},
+      {Mid::F, Mid::R, F32 ? 1850 : 620, F32 ? 1850 : 530, {1500, 5000, 1500}, true, false},
+      {Deep::F, Deep::R, F32 ? 1850 : 550, F32 ? 1850 : 550, {6000, 10000, 3000}, true, false},
+      {Plain::F, Plain::R, F32 ? 2100 : 600, F32 ? 2100 : 700, {1500, 5000, 1500}, false, true},
+      {Small::F, Small::R, F32 ? 690 : 290, F32 ? 630 : 220, {2200, 4000, 1000}, false, false},
+      {Tiny::F, Tiny::R, F32 ? 440 : 220, F32 ? 370 : 160, {1400, 2500, 700}, false, false},
+      {Least::F, Least::R, F32 ? 300 : 170, F32 ? 190 : 100, {0, 1300, 400}, false, false}};
+  const int64_t steps = ((int64_t)a.depth * (int64_t)sizeof(T) + kRow - 1) / kRow;
+  int pick = -1;
+  int64_t least_time = 0;
+  for (int i = 0; i < 8; ++i) {
+    const Cost &c = costs[i];
+    if ((c.wide && !(dma && near)) || (c.plain && dma && near)) continue;
+    if (i == 7 && EPI == EPI_GATE) continue;
+    const int64_t n = (tiles(c.f, c.r) + 255) / 256;
+    // (through registers, smaller tiles take half as long again)
+    const int64_t step = std::max<int64_t>(c.alone, n * c.busy) * (i > 4 && !dma ? 3 : 2) / 2;
+    const int64_t time = steps * step + n * c.finish[G];
+    if (pick < 0 || time < least_time) pick = i, least_time = time;
+  }
+  auto small = [&](auto tile) {
+    using TL = decltype(tile);
+    return dma ? launch<T, TL, EPI, true>(a, s) : launch<T, TL, EPI, false>(a, s);
+  };
+  switch (pick) {
+    case 0: return launch_wide<T, Big, EPI>(a, s);
+    case 1: return launch_wide<T, Half, EPI>(a, s);
+    case 2: return launch_wide<T, Mid, EPI>(a, s);
+    case 3: return launch_wide<T, Deep, EPI>(a, s);
+    case 4: return small(Plain());
+    case 5: return small(Small());
+    case 6: return small(Tiny());
+  }
+  if constexpr (EPI != EPI_GATE) return small(Least());
+  return LRCNN_OK;
 }
 
 template <int EPI>
