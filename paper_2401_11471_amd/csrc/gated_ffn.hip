@@ -13,6 +13,7 @@
 #include "kdev.hpp"
 
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 namespace lrcnn {
@@ -888,11 +889,15 @@ int launch_wide(FfnArgs &a, hipStream_t s) {
   return LRCNN_OK;
 }
 
+std::atomic<int> g_tile{-1};  // test hook: the variant to take where it can
+
 template <typename T, int EPI>
 int product(FfnArgs a, hipStream_t s) {
   constexpr int H = EPI == EPI_GATE ? 2 : 1;
+  constexpr int kFew = 8;  // number of the variant for few rows; the others: costs below
+  const int forced = g_tile;
   if constexpr (EPI != EPI_BACK) {
-    if (a.rows <= kFewRows && !a.ku.q && !a.kv.q) {
+    if (a.rows <= kFewRows && !a.ku.q && !a.kv.q && (forced < 0 || forced == kFew)) {
       const unsigned g = (unsigned)((a.feats + 15) / 16);
       if (a.rows <= 16) ffn_few_kernel<T, 1, EPI><<<g, 512, 0, s>>>(a);
       else ffn_few_kernel<T, 2, EPI><<<g, 512, 0, s>>>(a);
@@ -931,8 +936,12 @@ int product(FfnArgs a, hipStream_t s) {
   int64_t least_time = 0;
   for (int i = 0; i < 8; ++i) {
     const Cost &c = costs[i];
-    if ((c.wide && !(dma && near)) || (c.plain && dma && near)) continue;
+    if ((c.wide && !(dma && near)) || (c.plain && dma && near && forced != i)) continue;
     if (i == 7 && EPI == EPI_GATE) continue;
+    if (forced == i) {
+      pick = i;
+      break;
+    }
     const int64_t n = (tiles(c.f, c.r) + 255) / 256;
     // (through registers, smaller tiles take half as long again)
     const int64_t step = std::max<int64_t>(c.alone, n * c.busy) * (i > 4 && !dma ? 3 : 2) / 2;
@@ -983,6 +992,8 @@ using namespace lrcnn::act8;
     const int st_ = (x);               \
     if (st_ != LRCNN_OK) return st_;   \
   } while (0)
+
+extern "C" void lrcnn_debug_ffn_tile(int32_t tile) { g_tile = tile; }
 
 extern "C" int lrcnn_gated_ffn_forward(int64_t rows, int64_t n_in, int64_t hidden, int64_t n_out,
                                        int32_t dtype, int32_t kind, const void *x, int64_t ldx,

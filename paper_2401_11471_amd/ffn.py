@@ -18,8 +18,16 @@ after the first adds only what it keeps.
 The passes and the update of the weights run in the HIP library, the linear
 products and input gradients as 1x1 convolutions; the biases' and norms'
 updates and the weights' transposes are torch operations.
+
+``fused``: a gated block's products run as two kernels a pass, the activation in the
+first one's registers: u and v then never exist at full width, and a is formed from their
+float32 values. ``dropout``: y = norm2(x + dropout(z)), whose mask is drawn again in the
+backward pass from the generator's state in device memory. ``GroupNorm`` normalises and
+activates the trunk's map in front of the block.
+
 ``python -m paper_2401_11471_amd.ffn`` trains a small trunk, block and classifier
-head on random labelled images.
+head on random labelled images; with ``--fused`` the trunk's map is group-normalised, the
+block is fused and drops out a tenth.
 """
 from __future__ import annotations
 
@@ -101,6 +109,35 @@ class Norm:
         self.beta.sub_(lr * self.dbeta)
 
 
+class GroupNorm:
+    """Group norm with an activation over a map [batch * pixels][cols], whose backward
+    pass reads the checkpoint of the normalised map."""
+
+    def __init__(self, batch, pixels, cols, groups, kind, device="cuda"):
+        self.batch, self.groups, self.kind = batch, groups, kind
+        self.gamma = torch.ones(cols, device=device)
+        self.beta = torch.zeros(cols, device=device)
+        self.dgamma, self.dbeta = torch.empty(2, cols, device=device).unbind(0)
+        self.rstd = torch.empty(batch, groups, device=device)
+        self.ckpt = torch.empty(L.lrcnn_act8_bytes(batch * pixels, cols), device=device,
+                                dtype=torch.uint8)
+        self.ws = torch.empty(L.lrcnn_group_norm_workspace_bytes(batch, pixels, cols, groups),
+                              device=device, dtype=torch.uint8)
+
+    def forward(self, x, y):
+        L.lrcnn_group_norm_forward(self.kind, x, self.gamma, self.beta, EPS, y, self.batch,
+                                   self.groups, self.ws, rstd=self.rstd, ckpt=self.ckpt)
+
+    def backward(self, dy, dx):
+        L.lrcnn_group_norm_backward(self.kind, dy, self.rstd, self.gamma, self.beta, dx,
+                                    self.batch, self.groups, self.ws, dgamma=self.dgamma,
+                                    dbeta=self.dbeta, ckpt=self.ckpt)
+
+    def update(self, lr):
+        self.gamma.sub_(lr * self.dgamma)
+        self.beta.sub_(lr * self.dbeta)
+
+
 class Scratch:
     """Named byte buffers that blocks use within a pass and keep nothing in: one set
     for all blocks that run one after the other on one stream."""
@@ -112,20 +149,30 @@ class Scratch:
     def take(self, name, *shape, dtype=torch.uint8):
         """The head of a buffer as a tensor."""
         n = math.prod(shape) * dtype.itemsize
-        if n > self.buffers[name].numel():
-            raise ValueError(f"scratch for {name} has {self.buffers[name].numel()} bytes, "
-                             f"{n} needed: make the largest block first")
+        have = self.buffers[name].numel() if name in self.buffers else 0
+        if n > have:
+            raise ValueError(f"scratch for {name} has {have} bytes, {n} needed: make the largest "
+                             "block first, one with dropout before one without")
         return self.buffers[name][:n].view(dtype).view(shape)
 
 
 class FeedForward:
     """The block on [rows][cols] with `hidden` features in the middle. `scratch`: that
     of another block, at least as large, that runs before or after this one
-    on the same stream; None: its own."""
+    on the same stream; None: its own. `fused` (a gated block): two kernels a pass.
+    `dropout`: the share of z that is dropped; `rng` (int64 [2] on the device): seed and
+    offset of its generator, the offset advanced by the caller between steps, not between
+    a step's forward and backward pass; `site`: another number for each block of a
+    step."""
 
     def __init__(self, rows, cols, hidden, dtype=L.BF16, kind=L.ACT_GELU, gated=False,
-                 device="cuda", seed=0, scratch=None):
+                 device="cuda", seed=0, scratch=None, fused=False, dropout=0.0, rng=None, site=0):
+        if fused and not gated:
+            raise ValueError("a fused block is gated")
+        if dropout and rng is None:
+            raise ValueError("dropout needs rng")
         g = torch.Generator().manual_seed(seed)
+        self.fused, self.dropout, self.rng, self.site = fused, dropout, rng, site
         self.kind, self.gated, self.hidden = kind, gated, hidden
         wide = 2 * hidden if gated else hidden
         self.norm1, self.norm2 = Norm(rows, cols, device), Norm(rows, cols, device)
@@ -140,13 +187,15 @@ class FeedForward:
         layers = (self.norm1, self.norm2, self.lin1, self.lin2)
         tdt, n_ws = torch_dtype(dtype), max(layer.ws.numel() for layer in layers)
         full = {"h": cols, "z": cols, "u": wide, "a": hidden}
+        if dropout:
+            full["d"] = cols  # the gradient behind the dropout
         if scratch is None:
             sizes = {k: rows * w * tdt.itemsize for k, w in full.items()}
             sizes.update(k_a=L.lrcnn_act8_bytes(rows, hidden), ws=n_ws)
             scratch = Scratch(sizes, device)
         self.scratch = scratch
-        self.h, self.z, self.u, self.a = (scratch.take(k, rows, w, dtype=tdt)
-                                          for k, w in full.items())
+        self.h, self.z, self.u, self.a, *self.d = (scratch.take(k, rows, w, dtype=tdt)
+                                                   for k, w in full.items())
         self.k_a = scratch.take("k_a", L.lrcnn_act8_bytes(rows, hidden))
         scratch.take("ws", n_ws)
         for layer in layers:
@@ -164,21 +213,40 @@ class FeedForward:
     def forward(self, x, y):
         u, v = self._halves(self.u)
         self.norm1.forward(x, self.h)
-        self.lin1.forward(self.h, self.u)
-        L.lrcnn_activation_forward(self.kind, u, self.a, v=v, ckpt_u=self.k_u, ckpt_v=self.k_v)
-        self.lin2.forward(self.a, self.z)
-        self.norm2.forward(self.z, y, residual=x)
+        if self.fused:
+            L.lrcnn_gated_ffn_forward(self.kind, self.h, self.lin1.w, self.a, b1=self.lin1.b,
+                                      w2=self.lin2.w, b2=self.lin2.b, z=self.z, ckpt_u=self.k_u,
+                                      ckpt_v=self.k_v)
+        else:
+            self.lin1.forward(self.h, self.u)
+            L.lrcnn_activation_forward(self.kind, u, self.a, v=v, ckpt_u=self.k_u,
+                                       ckpt_v=self.k_v)
+            self.lin2.forward(self.a, self.z)
+        if self.dropout:
+            L.lrcnn_dropout(self.z, self.z, self.dropout, self.rng, residual=x, site=self.site)
+            self.norm2.forward(self.z, y)
+        else:
+            self.norm2.forward(self.z, y, residual=x)
 
     def backward(self, dy, dx):
         """dx from dy; the parameters' gradients stay with their layers."""
         du, dv = self._halves(self.u)
         dt, da, dh = self.z, self.a, self.h
         self.norm2.backward(dy, dt)
-        self.lin2.input_gradient(dt, da)
-        L.lrcnn_activation_backward(self.kind, da, du, ckpt_u=self.k_u, ckpt_v=self.k_v, dv=dv,
-                                    ckpt_a=self.k_a)
-        self.lin2.weight_gradient(dt, self.k_a)
-        self.lin1.input_gradient(self.u, dh)
+        dz = dt
+        if self.dropout:
+            dz = self.d[0]
+            L.lrcnn_dropout(dt, dz, self.dropout, self.rng, site=self.site)
+        if self.fused:
+            L.lrcnn_gated_ffn_backward(self.kind, dz, self.lin2.wt, self.u, ckpt_u=self.k_u,
+                                       ckpt_v=self.k_v, ckpt_a=self.k_a, w1t=self.lin1.wt, dx=dh)
+            self.lin2.weight_gradient(dz, self.k_a)
+        else:
+            self.lin2.input_gradient(dz, da)
+            L.lrcnn_activation_backward(self.kind, da, du, ckpt_u=self.k_u, ckpt_v=self.k_v,
+                                        dv=dv, ckpt_a=self.k_a)
+            self.lin2.weight_gradient(dz, self.k_a)
+            self.lin1.input_gradient(self.u, dh)
         self.lin1.weight_gradient(self.u, self.norm1.ckpt, self.norm1.gamma, self.norm1.beta)
         self.norm1.backward(dh, dx, dres=dt)
 
@@ -187,7 +255,7 @@ class FeedForward:
             layer.update(lr)
 
 
-def main():
+def main(fused=False):
     from .device import DeviceModel
     from .train import Trainer
     import numpy as np
@@ -206,16 +274,33 @@ def main():
     rows = batch * oh * ow
     fc = rng.standard_normal((classes, oh * ow * oc)) / math.sqrt(oh * ow * oc)
     tr = Trainer(plan, dm, fc, np.zeros(classes), rng.integers(0, classes, batch))
-    block = FeedForward(rows, oc, 4 * oc, L.BF16, L.ACT_SILU, gated=True)
+    more = {}
+    if fused:
+        state = torch.tensor([1, 0], device="cuda")
+        more = dict(fused=True, dropout=0.1, rng=state)
+        norm = GroupNorm(batch, oh * ow, oc, 8, L.ACT_SILU)
+        n, dn = (torch.empty(rows, oc, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    block = FeedForward(rows, oc, 4 * oc, L.BF16, L.ACT_SILU, gated=True, **more)
     y, dy, dx = (torch.empty(rows, oc, device="cuda", dtype=torch.bfloat16) for _ in range(3))
     full = 2 * rows * (3 * oc + 3 * 4 * oc)
     print(f"{rows} rows of {oc}: {block.saved_bytes()} bytes kept, {full} in bfloat16")
     for step in range(steps):
         L.lrcnn_forward_rows(plan, dm.x, dm.w, dm.sc, dm.sf, tr.y, tr.ws)
-        block.forward(tr.y.view(rows, oc), y)
+        x = tr.y.view(rows, oc)
+        if fused:
+            state[1] = step
+            norm.forward(x, n)
+            block.forward(n, y)
+        else:
+            block.forward(x, y)
         L.lrcnn_head_loss(plan, y, tr.fc_w, tr.fc_b, tr.labels, tr.logits, tr.loss, dy,
                           tr.d_fc_w, tr.d_fc_b, tr.head_ws)
-        block.backward(dy, dx)
+        if fused:
+            block.backward(dy, dn)
+            norm.backward(dn, dx)
+            norm.update(lr)
+        else:
+            block.backward(dy, dx)
         L.lrcnn_backward_rows(plan, dm.x, dm.w, dm.sc, dm.sf, dx, dm.dw, None, tr.ws)
         L.lrcnn_sgd_update(plan, lr, dm.w, dm.dw, tr.fc_w, tr.d_fc_w, tr.fc_b, tr.d_fc_b)
         block.update(lr)
@@ -224,4 +309,5 @@ def main():
 
 
 if __name__ == "__main__":
-    main()
+    import sys
+    main(fused="--fused" in sys.argv[1:])

@@ -151,6 +151,8 @@ def _load():
     lib.lrcnn_debug_fork_wgrad.restype = C.c_int
     lib.lrcnn_debug_dgrad_phases.argtypes = [C.c_int]
     lib.lrcnn_debug_dgrad_phases.restype = None
+    lib.lrcnn_debug_ffn_tile.argtypes = [i32]
+    lib.lrcnn_debug_ffn_tile.restype = None
     lib.lrcnn_debug_profile.argtypes = [C.c_int]
     lib.lrcnn_debug_profile.restype = None
     lib.lrcnn_debug_profile_collect.restype = C.c_int
@@ -184,7 +186,7 @@ EXPORTS = ("lrcnn_plan", "lrcnn_plan_query", "lrcnn_plan_node_shape",
            "lrcnn_backward_rows", "lrcnn_layerwise_reference_gpu", "lrcnn_last_error",
            "lrcnn_debug_dry_run", "lrcnn_debug_fp_pipeline", "lrcnn_debug_act_fusion",
            "lrcnn_debug_dgrad_phases", "lrcnn_debug_serial_wgrad",
-           "lrcnn_debug_fork_wgrad",
+           "lrcnn_debug_fork_wgrad", "lrcnn_debug_ffn_tile",
            "lrcnn_debug_profile",
            "lrcnn_debug_profile_collect", "lrcnn_debug_profile_entry",
            "lrcnn_debug_profile_roofline",
@@ -729,6 +731,12 @@ def lrcnn_debug_fork_wgrad(mode):
     in a captured graph; 1 all, 2 every other one). Returns how many went there
     since the last call."""
     return LIB.lrcnn_debug_fork_wgrad(int(mode))
+
+
+def lrcnn_debug_ffn_tile(tile):
+    """Test hook: the gated feed-forward block's tile (-1 by estimate; 0 .. 8 as the
+    header lists them, where the operands allow it)."""
+    LIB.lrcnn_debug_ffn_tile(tile)
 
 
 def lrcnn_debug_act_fusion(on):

@@ -209,11 +209,37 @@ def test_wide(rows, n_in, hidden, n_out, dtype):
     check_backward(rows, n_in, hidden, n_out, dtype, "relu", 8, 8, False)
 
 
-def test_rows_do_not_meet():
+@pytest.fixture
+def tile():
+    """Takes a variant of the products, and leaves the choice to the library after."""
+    yield L.lrcnn_debug_ffn_tile
+    L.lrcnn_debug_ffn_tile(-1)
+
+
+@TYPES
+@pytest.mark.parametrize("variant", range(9))
+def test_every_tile(variant, dtype, tile):
+    """Each variant at sizes that end inside its tiles, in one step and in many, aligned
+    and not, from checkpoints and full-width values."""
+    tile(variant)
+    tell("tile", variant)
+    for rows, n_in, hidden, n_out in [(300, 200, 152, 136), (130, 64, 288, 264), (33, 328, 40, 72)]:
+        if variant == 8:
+            rows = 29
+        check_forward(rows, n_in, hidden, n_out, dtype, "silu", 0, 0, variant != 8, True)
+        check_forward(rows, n_in, hidden, n_out, dtype, "gelu_tanh", 8, 8, variant != 8, False)
+        check_backward(rows, n_in, hidden, n_out, dtype, "silu", 0, 0, True)
+        check_backward(rows, n_in, hidden, n_out, dtype, "gelu", 8, 8, False)
+    check_forward(270, 77, 129, 65, dtype, "relu", 3, 1, variant != 8, True)
+    check_backward(270, 77, 129, 65, dtype, "silu", 3, 1, True)
+
+
+@pytest.mark.parametrize("variant", range(9))
+def test_rows_do_not_meet(variant, tile):
     """A row that is not finite spoils its own results alone, in every variant."""
-    for rows, n_in, hidden, n_out in [(20, 64, 48, 40), (100, 72, 70, 64), (2100, 72, 1000, 1040),
-                                      (4200, 72, 2080, 1100)]:
-        tell("rows", rows, n_in, hidden, n_out)
+    tile(variant)
+    for rows, n_in, hidden, n_out in [(20, 64, 48, 40), (300, 72, 200, 264)]:
+        tell("rows", variant, rows, n_in, hidden, n_out)
         _, s = case(rows, n_in, hidden, n_out, BF16, 5)
         x = s["x"].bfloat16()
         run = lambda: (torch.empty(rows, hidden, device="cuda", dtype=BF16),
