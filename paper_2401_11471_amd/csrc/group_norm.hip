@@ -31,7 +31,7 @@ namespace {
 
 constexpr int64_t kMaxImages = 1 << 20, kMaxChannels = 1 << 20;
 constexpr int kBatch = 8;         // pixels that a thread holds at a time
-constexpr int kLeast = 2;         // pixels a thread, where that gives the CUs work
+constexpr int kLeast = 2;         // pixels a thread, where the CUs have no work else
 constexpr int kUnits = 2048;      // blocks of a pass, where there are as many
 constexpr int kApplyPixels = 4;   // applying passes: pixels in flight a thread
 
@@ -48,6 +48,7 @@ struct GnArgs {
   const float *mean, *rstd;  // [batch][groups]
   float *mean_out, *rstd_out;
   float2 *part;          // [units][cols]
+  float2 *chan;          // [batch][cols]
   float2 *stat;          // [batch][groups]: (mean, rstd), backward the two means
   float *dgamma, *dbeta;
   int accumulate;
@@ -93,7 +94,7 @@ __device__ __forceinline__ void group8(const GnArgs &a, const float2 *stat, cons
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int c = min(q.c + i, a.cols - 1);
-    const float2 v = stat[q.b * a.groups + c / a.per];
+    const float2 v = stat[q.b * a.groups + fdiv_q((uint32_t)c, a.by_per)];
     s[i] = v.x, t[i] = v.y;
   }
 }
@@ -101,7 +102,7 @@ __device__ __forceinline__ void group8(const GnArgs &a, const float *stat, const
                                        float (&s)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    s[i] = stat[q.b * a.groups + min(q.c + i, a.cols - 1) / a.per];
+    s[i] = stat[q.b * a.groups + fdiv_q((uint32_t)min(q.c + i, a.cols - 1), a.by_per)];
 }
 
 // Joins the block's rows by halves, in LDS; the first row's threads have the result.
@@ -219,7 +220,7 @@ __global__ __launch_bounds__(1024) void gn_group_kernel(GnArgs a) {
   };
   double sum = 0;
 #pragma unroll 4
-  for (uint32_t e = threadIdx.x; e < all; e += 1024) {
+  for (uint32_t e = threadIdx.x; e < all; e += blockDim.x) {
     uint32_t s;
     const float2 v = at(e, s);
     sum += count(s) * v.x;
@@ -227,7 +228,7 @@ __global__ __launch_bounds__(1024) void gn_group_kernel(GnArgs a) {
   const double mean = block_sum(sum, red) * a.inv;
   double m2 = 0;
 #pragma unroll 4
-  for (uint32_t e = threadIdx.x; e < all; e += 1024) {
+  for (uint32_t e = threadIdx.x; e < all; e += blockDim.x) {
     uint32_t s;
     const float2 v = at(e, s);
     const double d = v.x - mean;
@@ -378,6 +379,49 @@ __global__ __launch_bounds__(256) void gn_sums_kernel(GnArgs a) {
   }
 }
 
+// A channel's slabs joined to one entry [image][channel], 32 channels a block of an
+// image: for groups whose slabs and channels are too many for the block that joins a group.
+// SUMS: sums, else mean and centred sum of squares.
+template <bool SUMS>
+__global__ __launch_bounds__(1024) void gn_channel_kernel(GnArgs a, float2 *out) {
+  __shared__ double l1[32][33], l2[32][33];
+  const uint32_t blocks = (uint32_t)(a.cols + 31) / 32, b = blockIdx.x / blocks;
+  const int x = threadIdx.x & 31, r = threadIdx.x >> 5, c = (int)(blockIdx.x - b * blocks) * 32 + x;
+  const float2 *part = a.part + (int64_t)b * a.slabs * a.cols + c;
+  auto count = [&](int s) { return (double)min(a.slab, a.pixels - s * a.slab); };
+  // the sums over r of the threads of a column, the same in each
+  auto total = [&](double (&l)[32][33], double v) {
+    l[r][x] = v;
+    __syncthreads();
+    double t = 0;
+    for (int k = 0; k < 32; ++k) t += l[k][x];
+    return t;
+  };
+  double s1 = 0, s2 = 0;
+  if (c < a.cols) {
+#pragma unroll 4
+    for (int s = r; s < a.slabs; s += 32) {
+      const float2 v = part[(int64_t)s * a.cols];
+      s1 += SUMS ? v.x : count(s) * v.x;
+      if (SUMS) s2 += v.y;
+    }
+  }
+  s1 = total(l1, s1);
+  if constexpr (!SUMS) {
+    s1 /= (double)a.pixels;
+    if (c < a.cols) {
+#pragma unroll 4
+      for (int s = r; s < a.slabs; s += 32) {
+        const float2 v = part[(int64_t)s * a.cols];
+        const double d = v.x - s1;
+        s2 += v.y + count(s) * d * d;
+      }
+    }
+  }
+  s2 = total(l2, s2);
+  if (r == 0 && c < a.cols) out[(int64_t)b * a.cols + c] = make_float2((float)s1, (float)s2);
+}
+
 // dgamma and dbeta of 32 channels: thread (r, c) takes every 32nd unit from r on, the
 // 32 sums joined in order.
 __device__ __forceinline__ void channel_grads(const GnArgs &a, int block) {
@@ -416,7 +460,7 @@ __global__ __launch_bounds__(1024) void gn_join_kernel(GnArgs a) {
   const float2 *part = a.part + b * a.slabs * (int64_t)a.cols + (int64_t)g * a.per;
   double s1 = 0, s2 = 0;
 #pragma unroll 4
-  for (uint32_t e = threadIdx.x; e < all; e += 1024) {
+  for (uint32_t e = threadIdx.x; e < all; e += blockDim.x) {
     uint32_t s, c;
     fdiv_qr(e, a.by_per, s, c);
     const float2 v = part[(int64_t)s * a.cols + c];
@@ -477,11 +521,13 @@ __device__ __forceinline__ Whole whole(const GnArgs &a) {
   return w;
 }
 // Sums of M values a channel over the block's rows, then over each group's channels
-// weighted by `weigh`, of the channel within the block. chan [waves][M][8 tpr]: each channel's sums of a wave; the
-// waves and channels are added in 64 bits, by 16 threads a group, the first of which
-// makes of them what all threads find in stat[local group] (64-bit division and roots
-// by every thread take longer than the rest of a small call).
+// weighted by `weigh`, of the channel within the block. chan [waves][M][8 tpr]: each
+// channel's sums of a wave, then of the block in [M][8 tpr]; the channels are added in
+// 64 bits, by 16 or 64 threads a group, the first of which makes of them what all
+// threads find in stat[local group].
 constexpr int kWide = 512;  // channels of a block at most
+// Waves whose sums of a channel are still apart in chan after group_sums' first step
+__device__ __forceinline__ int waves_left() { return blockDim.x > 256 ? 1 : blockDim.x >> 6; }
 template <int M, typename F, typename G>
 __device__ __forceinline__ void group_sums(const GnArgs &a, const Whole &w, float (&v)[M][8],
                                            float *chan, float2 *stat, F &&weigh, G &&make) {
@@ -501,25 +547,37 @@ __device__ __forceinline__ void group_sums(const GnArgs &a, const Whole &w, floa
       for (int i = 0; i < 8; ++i) chan[(wave * M + m) * wide + lane * 8 + i] = v[m][i];
   }
   __syncthreads();
-  const int here = min(a.width, a.cols - w.c0) / a.per;
-  const int all = waves * a.per;
-  for (int g = threadIdx.x >> 4; g < here; g += blockDim.x >> 4) {
+  // many waves' in order, one thread a channel and value; the first wave's place takes them
+  const int left = waves_left();
+  if (left == 1) {
+    for (int c = threadIdx.x; c < M * wide; c += blockDim.x) {
+      float t = chan[c];
+#pragma unroll 4
+      for (int k = 1; k < waves; ++k) t += chan[k * M * wide + c];
+      chan[c] = t;
+    }
+    __syncthreads();
+  }
+  const int here = (int)fdiv_q((uint32_t)min(a.width, a.cols - w.c0), a.by_per);
+  // (one group a wave while there are waves for all, else four)
+  const int lanes = here <= waves ? 64 : 16, in = threadIdx.x & (lanes - 1);
+  for (int g = threadIdx.x / lanes; g < here; g += blockDim.x / lanes) {
     double t[M];
 #pragma unroll
     for (int m = 0; m < M; ++m) t[m] = 0;
-#pragma unroll 4
-    for (int e = threadIdx.x & 15; e < all; e += 16) {
-      uint32_t wv, c;
-      fdiv_qr((uint32_t)e, a.by_per, wv, c);
-      const int ch = g * a.per + (int)c;
-      const double wt = weigh(ch);
+    for (int c = g * a.per + in; c < (g + 1) * a.per; c += lanes) {
+      const double wt = weigh(c);
 #pragma unroll
-      for (int m = 0; m < M; ++m) t[m] += wt * chan[(wv * M + m) * wide + ch];
+      for (int m = 0; m < M; ++m) {
+        float x = chan[m * wide + c];
+        for (int k = 1; k < left; ++k) x += chan[(k * M + m) * wide + c];
+        t[m] += wt * x;
+      }
     }
 #pragma unroll
     for (int m = 0; m < M; ++m)
-      for (int s = 1; s < 16; s *= 2) t[m] += __shfl_xor(t[m], s);
-    if ((threadIdx.x & 15) == 0) make(g, t);
+      for (int s = 1; s < lanes; s *= 2) t[m] += __shfl_xor(t[m], s);
+    if (in == 0) make(g, t);
   }
   __syncthreads();
 }
@@ -669,10 +727,11 @@ __global__ __launch_bounds__(1024) void gn_whole_back_kernel(GnArgs a) {
                 });
   // the image's sums of each channel, for dgamma and dbeta
   if (a.part) {
-    const int waves = blockDim.x >> 6, here = min(a.width, a.cols - w.c0);
+    const int here = min(a.width, a.cols - w.c0);
     for (int c = threadIdx.x; c < here; c += blockDim.x) {
-      float s1 = 0.f, s2 = 0.f;
-      for (int k = 0; k < waves; ++k) s1 += chan[2 * k * wide + c], s2 += chan[(2 * k + 1) * wide + c];
+      float s1 = chan[c], s2 = chan[wide + c];
+      for (int k = 1; k < waves_left(); ++k)
+        s1 += chan[2 * k * wide + c], s2 += chan[(2 * k + 1) * wide + c];
       if (a.batch == 1) {
         const int at = w.c0 + c;
         if (a.dbeta) a.dbeta[at] = a.accumulate ? a.dbeta[at] + s1 : s1;
@@ -713,10 +772,12 @@ Split split_of(int64_t batch, int64_t pixels, int64_t cols) {
   while (s.tpr < 64 && s.tpr < vecs) s.tpr *= 2;
   s.ctiles = (int)up(vecs, s.tpr);
   pixels = std::max<int64_t>(pixels, 1);
-  const int64_t by_pixels = up(pixels, 256 / s.tpr * kLeast);  // pixels worth a block
-  const int64_t units = std::max<int64_t>(kUnits / s.ctiles, 1);
-  s.slab = up(pixels, std::max<int64_t>(
-                          std::min(units / std::max<int64_t>(batch, 1), by_pixels), 1));
+  batch = std::max<int64_t>(batch, 1);
+  // (a thread's eight channels' constants take as long as a few pixels)
+  auto cut = [&](int64_t blocks, int64_t least) {
+    return std::min(blocks / s.ctiles / batch, up(pixels, 256 / s.tpr * least));
+  };
+  s.slab = up(pixels, std::max<int64_t>(std::max(cut(kUnits, kBatch), cut(kUnits / 4, kLeast)), 1));
   s.slabs = up(pixels, s.slab);
   return s;
 }
@@ -755,11 +816,13 @@ Block block_of(int64_t batch, int64_t pixels, int64_t cols, int64_t per, int es,
   return best;
 }
 
-size_t part_bytes(int64_t batch, int64_t cols) {
-  return a256((size_t)most_units(batch, cols) * (size_t)cols * 8);
+size_t part_bytes(int64_t units, int64_t cols) {
+  return a256((size_t)units * (size_t)cols * 8);
 }
+// units' channels, images' channels, images' groups
 size_t need_bytes(int64_t batch, int64_t cols, int64_t groups) {
-  return part_bytes(batch, cols) + a256((size_t)batch * (size_t)groups * 8);
+  return part_bytes(most_units(batch, cols), cols) + part_bytes(batch, cols) +
+         a256((size_t)batch * (size_t)groups * 8);
 }
 
 int gn_shape(int64_t batch, int64_t pixels, int64_t channels, int64_t groups, int32_t dtype) {
@@ -791,7 +854,8 @@ int gn_args(int64_t batch, int64_t pixels, int64_t channels, int64_t groups, voi
   a->by_per = fast_div((uint32_t)a->per);
   a->inv = 1.0 / ((double)pixels * (double)a->per);
   a->part = (float2 *)ws;
-  a->stat = (float2 *)((char *)ws + part_bytes(batch, channels));
+  a->chan = (float2 *)((char *)ws + part_bytes(most_units(batch, channels), channels));
+  a->stat = (float2 *)((char *)a->chan + part_bytes(batch, channels));
   return LRCNN_OK;
 }
 // The passes over slabs
@@ -799,6 +863,23 @@ void cut(GnArgs *a) {
   const Split s = split_of(a->batch, a->pixels, a->cols);
   a->slab = s.slab, a->slabs = (int)s.slabs, a->units = a->batch * s.slabs;
   a->tpr = s.tpr, a->ctiles = s.ctiles;
+}
+
+// The arguments of the kernel that joins by group: where a group has many slabs and
+// channels these are joined by channel first (one block of 1024 threads reads 850000
+// entries, 512 slabs of 1659 channels, in 130 us).
+template <bool SUMS>
+GnArgs by_channel(GnArgs a, hipStream_t s) {
+  if ((int64_t)a.slabs * a.per <= 32768) return a;
+  gn_channel_kernel<SUMS><<<(unsigned)(a.batch * up(a.cols, 32)), 1024, 0, s>>>(a, a.chan);
+  a.part = a.chan, a.slabs = 1, a.slab = a.pixels, a.units = a.batch;
+  return a;
+}
+// Threads that join a group
+unsigned join_threads(const GnArgs &a) {
+  unsigned t = 64;
+  while (t < 1024 && t * 2 < (int64_t)a.slabs * a.per) t *= 2;
+  return t;
 }
 
 unsigned blocks_of(GnArgs *a, const Block &b) {
@@ -878,7 +959,8 @@ extern "C" int lrcnn_group_norm_forward(int64_t batch, int64_t pixels, int64_t c
       cut(&w);
       const unsigned grid = (unsigned)(w.units * w.ctiles);
       gn_stats_kernel<T><<<grid, 256, 0, s>>>(w);
-      gn_group_kernel<<<(unsigned)(batch * groups), 1024, 0, s>>>(w);
+      const GnArgs j = by_channel<false>(w, s);
+      gn_group_kernel<<<(unsigned)(batch * groups), join_threads(j), 0, s>>>(j);
       gn_apply_kernel<T, K.value><<<grid, 256, 0, s>>>(w);
     };
     if (dtype == LRCNN_BF16) run((bf16 *)nullptr);
@@ -947,7 +1029,13 @@ extern "C" int lrcnn_group_norm_backward(int64_t batch, int64_t pixels, int64_t 
       cut(&w);
       const unsigned grid = (unsigned)(w.units * w.ctiles);
       gn_sums_kernel<T, K.value, ck.value><<<grid, 256, 0, s>>>(w);
-      gn_join_kernel<<<(unsigned)(batch * groups) + (grads ? chans : 0), 1024, 0, s>>>(w);
+      const GnArgs j = by_channel<true>(w, s);
+      if (join_threads(j) == 1024 || batch * groups < 512) {
+        gn_join_kernel<<<(unsigned)(batch * groups) + (grads ? chans : 0), 1024, 0, s>>>(j);
+      } else {
+        gn_join_kernel<<<(unsigned)(batch * groups), join_threads(j), 0, s>>>(j);
+        if (grads) gn_grads_kernel<<<chans, 1024, 0, s>>>(j);
+      }
       gn_dx_kernel<T, K.value, ck.value><<<grid, 256, 0, s>>>(w);
     };
     auto typed = [&](auto *t) {
