@@ -745,29 +745,34 @@ __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(F
   }
 }
 
-// Few rows (up to 16 NC): the weights' bytes bound it. 16 features (of u and of v) a
-// workgroup, eight waves that take turns along the depth, 128 bytes of a weight
-// row a step, straight into registers.
-template <typename T, int NC, int EPI>
+// Few rows (up to 16 NC): the weights' bytes bound it. 16 NF features (EPI_GATE: of u and
+// of v) a workgroup, eight waves that take turns along the depth, 128 bytes of a weight
+// row a step, straight into registers. NF 1 where that is all, 2 where checkpoints
+// are written or read: their groups of 32 leave by a strip.
+template <typename T, int NC, int EPI, int NF>
 __global__ __launch_bounds__(512) void ffn_few_kernel(FfnArgs a) {
   constexpr int E = 16 / (int)sizeof(T), BK = kRow / (int)sizeof(T);
-  constexpr int H = EPI == EPI_GATE ? 2 : 1, W = 8, U = 4 / H;
-  __shared__ float red[W][H][NC][64][4];
+  constexpr int H = EPI == EPI_GATE ? 2 : 1, W = 8, U = 4 / (H * NF);
+  __shared__ float red[W][H][NF][NC][64][4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int f0 = blockIdx.x * 16, g = lane >> 4;
-  const int f = min(f0 + (lane & 15), a.feats - 1);
-  const T *w[H], *x[NC];
+  const int f0 = blockIdx.x * 16 * NF, g = lane >> 4;
+  const T *w[H][NF], *x[NC];
 #pragma unroll
   for (int h = 0; h < H; ++h)
-    w[h] = (const T *)a.w + (f + (int64_t)h * a.feats) * a.depth + g * 2 * E;
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+      w[h][f] = (const T *)a.w + g * 2 * E +
+                (min(f0 + 16 * f + (lane & 15), a.feats - 1) + (int64_t)h * a.feats) * a.depth;
 #pragma unroll
   for (int c = 0; c < NC; ++c)
     x[c] = (const T *)a.x.p + (int64_t)min(16 * c + (lane & 15), a.rows - 1) * a.x.ld + g * 2 * E;
-  f32x4 acc[H][NC];
+  f32x4 acc[H][NF][NC];
 #pragma unroll
   for (int h = 0; h < H; ++h)
 #pragma unroll
-    for (int c = 0; c < NC; ++c) acc[h][c] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) acc[h][f][c] = (f32x4){0.f, 0.f, 0.f, 0.f};
   auto load = [&](const T *p, int n, auto whole) -> u32x4 {
     if constexpr (sizeof(T) == 2) {
       if constexpr (decltype(whole)::value) return __builtin_bit_cast(u32x4, *(const u32x4_a2 *)p);
@@ -783,17 +788,30 @@ __global__ __launch_bounds__(512) void ffn_few_kernel(FfnArgs a) {
   // N steps, W apart, from depth k on
   auto some = [&](int k, auto whole, auto many) {
     constexpr int N = decltype(many)::value;
-    u32x4 fw[N][H][2], fx[N][NC][2];
+    u32x4 fw[N][H][NF][2], fx[N][NC][2];
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
         const int at = k + n * W * BK + q * E, left = a.depth - at - g * 2 * E;
 #pragma unroll
-        for (int h = 0; h < H; ++h) fw[n][h][q] = load(w[h] + at, left, whole);
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int f = 0; f < NF; ++f) fw[n][h][f][q] = load(w[h][f] + at, left, whole);
 #pragma unroll
         for (int c = 0; c < NC; ++c) fx[n][c][q] = load(x[c] + at, left, whole);
       }
+    auto one = [&](f32x4 &d, u32x4 p, u32x4 q) {
+      if constexpr (sizeof(T) == 2) {
+        d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, p),
+                                                    __builtin_bit_cast(bf16x8, q), d, 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          d = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(p[e]), __uint_as_float(q[e]), d,
+                                                   0, 0, 0);
+      }
+    };
 #pragma unroll
     for (int n = 0; n < N; ++n)
 #pragma unroll
@@ -801,19 +819,9 @@ __global__ __launch_bounds__(512) void ffn_few_kernel(FfnArgs a) {
 #pragma unroll
         for (int h = 0; h < H; ++h)
 #pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            if constexpr (sizeof(T) == 2) {
-              acc[h][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                  __builtin_bit_cast(bf16x8, fw[n][h][q]), __builtin_bit_cast(bf16x8, fx[n][c][q]),
-                  acc[h][c], 0, 0, 0);
-            } else {
+          for (int f = 0; f < NF; ++f)
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                acc[h][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                    __uint_as_float(fw[n][h][q][e]), __uint_as_float(fx[n][c][q][e]), acc[h][c], 0,
-                    0, 0);
-            }
-          }
+            for (int c = 0; c < NC; ++c) one(acc[h][f][c], fw[n][h][f][q], fx[n][c][q]);
   };
   int k = wave * BK;
   for (; k + ((U - 1) * W + 1) * BK <= a.depth; k += U * W * BK)
@@ -824,33 +832,53 @@ __global__ __launch_bounds__(512) void ffn_few_kernel(FfnArgs a) {
 #pragma unroll
   for (int h = 0; h < H; ++h)
 #pragma unroll
-    for (int c = 0; c < NC; ++c) *(f32x4 *)red[wave][h][c][lane] = acc[h][c];
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) *(f32x4 *)red[wave][h][f][c][lane] = acc[h][f][c];
   __syncthreads();
-  for (int t = threadIdx.x; t < 256 * NC; t += 512) {
-    const int ft = t & 15, row = t >> 4, c = row >> 4, l = (ft >> 2) * 16 + (row & 15);
-    if (row >= a.rows || f0 + ft >= a.feats) continue;
-    float s[H];
+  if constexpr (NF == 2) {
+    __shared__ __align__(16) char strip_[32 * 32 * H * 4];
+    lds_char *const strip = (lds_char *)strip_;
+    for (int t = threadIdx.x; t < H * 2 * NC * 64; t += 512) {
+      const int l = t & 63, c = t / 64 % NC, f = t / (64 * NC) % 2, h = t / (128 * NC);
+      f32x4 s = *(const f32x4 *)red[0][h][f][c][l];
 #pragma unroll
-    for (int h = 0; h < H; ++h) {
-      s[h] = 0.f;
-#pragma unroll
-      for (int i = 0; i < W; ++i) s[h] += red[i][h][c][l][ft & 3];
-      if (a.bias) s[h] += a.bias[h * a.feats + f0 + ft];
+      for (int i = 1; i < W; ++i) s += *(const f32x4 *)red[i][h][f][c][l];
+      *(lds_f32x4 *)slot_of<H>(strip, 16 * c + (l & 15), 8 * h + 4 * f + (l >> 4)) = s;
     }
-    if constexpr (EPI == EPI_GATE) {
-      if (a.uv.p) {
-        T *p = (T *)a.uv.p + row * a.uv.ld + f0 + ft;
-        put(p, s[0]);
-        put(p + a.feats, s[1]);
+    __syncthreads();
+    if (wave) return;
+    const int c = f0 + 8 * (lane % Lanes<EPI, H>::PER);
+    Bias bias;
+    bias.load<EPI>(a, c);
+    strip_rows<T, EPI, H>(a, strip, 0, f0, bias, [&](int row, float (&u)[8], float (&v)[8]) {
+      read_uv<T>(a, row, c, u, v);
+    });
+  } else {
+    for (int t = threadIdx.x; t < 256 * NC; t += 512) {
+      const int ft = t & 15, row = t >> 4, c = row >> 4, l = (ft >> 2) * 16 + (row & 15);
+      if (row >= a.rows || f0 + ft >= a.feats) continue;
+      float s[H];
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        s[h] = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) s[h] += red[i][h][0][c][l][ft & 3];
+        if (a.bias) s[h] += a.bias[h * a.feats + f0 + ft];
       }
-      float fu = 0.f, df;
-      if (a.kind == LRCNN_ACT_SILU) activate<LRCNN_ACT_SILU>(s[0], fu, df);
-      else if (a.kind == LRCNN_ACT_GELU) activate<LRCNN_ACT_GELU>(s[0], fu, df);
-      else if (a.kind == LRCNN_ACT_GELU_TANH) activate<LRCNN_ACT_GELU_TANH>(s[0], fu, df);
-      else activate<LRCNN_ACT_RELU>(s[0], fu, df);
-      s[0] = fu * s[1];
+      if constexpr (EPI == EPI_GATE) {
+        if (a.uv.p) {
+          T *p = (T *)a.uv.p + row * a.uv.ld + f0 + ft;
+          put(p, s[0]);
+          put(p + a.feats, s[1]);
+        }
+        float fu[1], df[1];
+        const float u[1] = {s[0]};
+        activate_all(a.kind, u, fu, df);
+        s[0] = fu[0] * s[1];
+      }
+      put((T *)a.out.p + row * a.out.ld + f0 + ft, s[0]);
     }
-    put((T *)a.out.p + row * a.out.ld + f0 + ft, s[0]);
   }
 }
 
@@ -896,13 +924,18 @@ int product(FfnArgs a, hipStream_t s) {
   constexpr int H = EPI == EPI_GATE ? 2 : 1;
   constexpr int kFew = 8;  // number of the variant for few rows; the others: costs below
   const int forced = g_tile;
-  if constexpr (EPI != EPI_BACK) {
-    if (a.rows <= kFewRows && !a.ku.q && !a.kv.q && (forced < 0 || forced == kFew)) {
-      const unsigned g = (unsigned)((a.feats + 15) / 16);
-      if (a.rows <= 16) ffn_few_kernel<T, 1, EPI><<<g, 512, 0, s>>>(a);
-      else ffn_few_kernel<T, 2, EPI><<<g, 512, 0, s>>>(a);
+  if (a.rows <= kFewRows && (forced < 0 || forced == kFew)) {
+    auto few = [&](auto nc, auto nf) {
+      const unsigned g = (unsigned)((a.feats + 16 * nf.value - 1) / (16 * nf.value));
+      ffn_few_kernel<T, nc.value, EPI, nf.value><<<g, 512, 0, s>>>(a);
       return LRCNN_OK;
-    }
+    };
+    using std::integral_constant;
+    const integral_constant<int, 1> one;
+    const integral_constant<int, 2> two;
+    if constexpr (EPI != EPI_PLAIN)
+      if (EPI == EPI_BACK || a.ku.q || a.kv.q) return a.rows <= 16 ? few(one, two) : few(two, two);
+    if constexpr (EPI != EPI_BACK) return a.rows <= 16 ? few(one, one) : few(two, one);
   }
   constexpr int E = 16 / (int)sizeof(T);
   const bool dma = ((uintptr_t)a.x.p | (uintptr_t)a.w) % 16 == 0 && a.x.ld % E == 0 &&
