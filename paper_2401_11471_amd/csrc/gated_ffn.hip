@@ -893,26 +893,24 @@ typedef Tile<1, 2, 1, 1, 4, 3> Tiny;   // 64 x 32
 typedef Tile<1, 1, 1, 1, 4, 3> Least;  // 32 x 32, one block of features
 constexpr int kFewRows = 32;
 
-int lay_out(FfnArgs &a, int rows, int feats) {
+// Tiles that a grid takes (2^32 threads)
+constexpr int64_t kMostTiles = 1 << 22;
+void lay_out(FfnArgs &a, int rows, int feats) {
   a.gx = (a.rows + rows - 1) / rows;
   a.gy = (a.feats + feats - 1) / feats;
-  if ((int64_t)a.gx * a.gy > 1 << 22) return refuse(LRCNN_ESHAPE, "gated_ffn: too many tiles");
   a.panel = fast_div(8 * (uint32_t)a.gy);
   a.rest = fast_div((uint32_t)std::max(a.gx & 7, 1));
-  return LRCNN_OK;
 }
 template <typename T, typename TL, int EPI, bool DMA>
 int launch(FfnArgs &a, hipStream_t s) {
-  const int st = lay_out(a, TL::R, EPI == EPI_GATE ? TL::F / 2 : TL::F);
-  if (st != LRCNN_OK) return st;
+  lay_out(a, TL::R, EPI == EPI_GATE ? TL::F / 2 : TL::F);
   ffn_kernel<T, TL, EPI, DMA><<<(unsigned)(a.gx * a.gy), TL::THREADS, 0, s>>>(a);
   return LRCNN_OK;
 }
 
 template <typename T, typename W, int EPI>
 int launch_wide(FfnArgs &a, hipStream_t s) {
-  const int st = lay_out(a, W::R, EPI == EPI_GATE ? W::F / 2 : W::F);
-  if (st != LRCNN_OK) return st;
+  lay_out(a, W::R, EPI == EPI_GATE ? W::F / 2 : W::F);
   ffn_wide_kernel<T, W, EPI><<<(unsigned)(a.gx * a.gy), 256, 0, s>>>(a);
   return LRCNN_OK;
 }
@@ -970,7 +968,7 @@ int product(FfnArgs a, hipStream_t s) {
   for (int i = 0; i < 8; ++i) {
     const Cost &c = costs[i];
     if ((c.wide && !(dma && near)) || (c.plain && dma && near && forced != i)) continue;
-    if (i == 7 && EPI == EPI_GATE) continue;
+    if ((i == 7 && EPI == EPI_GATE) || tiles(c.f, c.r) > kMostTiles) continue;
     if (forced == i) {
       pick = i;
       break;
@@ -1004,12 +1002,16 @@ int run(int32_t dtype, const FfnArgs &a, void *stream) {
                              : product<float, EPI>(a, (hipStream_t)stream);
 }
 
+// n: the block's input or output features. The products that this call makes with them
+// have at most 2 hidden or n features.
 int ffn_shape(int64_t rows, int64_t n, int64_t hidden, int32_t dtype, int32_t kind) {
   const int st = take_shape(rows, n, dtype);
   if (st != LRCNN_OK) return st;
   if (hidden < 1) return refuse(LRCNN_ESHAPE, "need hidden >= 1");
   if (n > kMaxFeatures || hidden > kMaxFeatures / 2 || rows > kMaxFfnRows)
     return refuse(LRCNN_ESHAPE, "gated_ffn takes at most 2^24 features and 2^30 rows");
+  if (((rows + 127) / 128) * ((std::max(n, 2 * hidden) + 127) / 128) > kMostTiles)
+    return refuse(LRCNN_ESHAPE, "gated_ffn takes at most 2^22 tiles of 128 x 128");
   if (kind < LRCNN_ACT_RELU || kind > LRCNN_ACT_SILU)
     return refuse(LRCNN_EINVAL, "unknown activation");
   return LRCNN_OK;

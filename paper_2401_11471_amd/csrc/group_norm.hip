@@ -667,7 +667,8 @@ __global__ __launch_bounds__(1024) void gn_whole_kernel(GnArgs a) {
   if (a.gamma && w.n > 0) load8(a.gamma + w.c, w.n).get(ga);
   if (a.beta && w.n > 0) load8(a.beta + w.c, w.n).get(be);
   // (with a checkpoint the block's channels start and end with its groups of 32)
-  if (w.c >= (a.k.q ? min(a.pitch, w.c0 + (int)((a.width + kGroup - 1) / kGroup * kGroup)) : w.c0 + a.width)) return;
+  const int wide_end = w.c0 + (a.k.q ? (a.width + kGroup - 1) / kGroup * kGroup : a.width);
+  if (w.c >= wide_end || w.c >= a.pitch) return;
 #pragma unroll
   for (int j = 0; j < R; ++j) {
     const int64_t p = w.row + (int64_t)j * w.rows;
@@ -870,7 +871,7 @@ void cut(GnArgs *a) {
 // entries, 512 slabs of 1659 channels, in 130 us).
 template <bool SUMS>
 GnArgs by_channel(GnArgs a, hipStream_t s) {
-  if ((int64_t)a.slabs * a.per <= 32768) return a;
+  if (a.slabs == 1 || (int64_t)a.slabs * a.per <= 32768) return a;
   gn_channel_kernel<SUMS><<<(unsigned)(a.batch * up(a.cols, 32)), 1024, 0, s>>>(a, a.chan);
   a.part = a.chan, a.slabs = 1, a.slab = a.pixels, a.units = a.batch;
   return a;

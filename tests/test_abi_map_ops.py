@@ -134,7 +134,8 @@ def test_gated_ffn_refuses(call):
     assert call(dtype=3) == EDTYPE
     for kw in (dict(rows=-1), dict(n_in=0), dict(hidden=0), dict(n_out=0),
                dict(hidden=(1 << 23) + 1), dict(n_in=(1 << 24) + 1), dict(n_out=(1 << 24) + 1),
-               dict(rows=(1 << 30) + 1)):
+               dict(rows=(1 << 30) + 1), dict(rows=1 << 30, hidden=1 << 12),
+               dict(rows=1 << 26, n_in=1 << 14, n_out=1 << 14)):
         assert call(**kw) == ESHAPE, kw
     for kind in (-1, 4):
         assert call(kind=kind) == EINVAL

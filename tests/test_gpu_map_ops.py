@@ -31,7 +31,8 @@ KINDS = {"none": L.ACT_NONE, "relu": L.ACT_RELU, "gelu": L.ACT_GELU, "gelu_tanh"
 # batch, pixels, channels, groups
 SHAPES = [(1, 1, 1, 1), (1, 1, 8, 8), (3, 1, 12, 4), (2, 2, 7, 7), (2, 5, 30, 2), (1, 49, 512, 32),
           (7, 169, 510, 34), (2, 300, 96, 8), (5, 33, 33, 1), (1, 1000, 20, 20), (3, 130, 2048, 32),
-          (2, 777, 1100, 11), (130, 9, 40, 5), (1, 3000, 64, 1), (9, 64, 64, 16), (2, 17, 5000, 4)]
+          (2, 777, 1100, 11), (130, 9, 40, 5), (1, 3000, 64, 1), (9, 64, 64, 16), (2, 17, 5000, 4),
+          (150, 100, 512, 1), (3, 2047, 32, 2), (40, 60, 500, 1), (1, 900, 1659, 1), (20, 33, 416, 13)]
 SIZES = pytest.mark.parametrize("batch,pixels,cols,groups", SHAPES)
 
 
@@ -264,6 +265,28 @@ def test_group_norm_backward_by_differences():
             lo = f()
             flat[i] = old
             assert abs((hi - lo) / (2 * eps) - float(grad[i])) < 5e-3
+
+
+def test_group_norm_of_many_images():
+    """As many images and groups as a call takes."""
+    batch, cols, groups = 1 << 18, 256, 8
+    tell("group norm of many images")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(batch, cols, generator=g, device="cuda").bfloat16()
+    y, ws = torch.empty_like(x), workspace(batch, 1, cols, groups)
+    rstd = torch.empty(batch, groups, device="cuda")
+    L.lrcnn_group_norm_forward(L.ACT_NONE, x, None, None, 1e-5, y, batch, groups, ws, rstd=rstd)
+    at = [0, 1, 199999, batch - 1]
+    ref = OM.group_norm(np64(x[at]), 4, groups, 1.0, 0.0, np.float64(np.float32(1e-5)), "none")
+    close(y[at], ref[0], 64 * U * np.abs(ref[0]) + 1e-5, BF16)
+    close(rstd[at], ref[4], 22 * U * ref[4])
+    dx = torch.empty_like(x)
+    dg = torch.empty(cols, device="cuda")
+    mean = x.float().view(batch, groups, -1).mean(2)
+    L.lrcnn_group_norm_backward(L.ACT_NONE, y, rstd, None, None, dx, batch, groups, ws, dgamma=dg,
+                                x=x, mean=mean)
+    want = (y.double() * y.double()).sum(0)  # xh is y but for y's rounding, 2^-9 of it
+    assert ((dg.double() - want).abs() <= 2.0 ** -8 * want).all()
 
 
 def test_group_norm_without_rows():
