@@ -89,8 +89,8 @@ int lrcnn_debug_profile_roofline(int32_t i, double *bytes, double *roofline_ms);
 
 /* Tile of the gated feed-forward block's products: -1 (default) by estimated time,
  * else, where the operands allow it, 0 256 x 256, 1 256 x 128, 2 and 3 128 x 128
- * (two workgroups a CU, one), 4 128 x 128 through registers, 5 64 x 64,
- * 6 64 x 32, 7 32 x 32 (not the forward pass' first product), 8 up to 32 rows. */
+ * (two workgroups a CU, one), 4 64 x 64, 5 64 x 32, 6 32 x 32 (not the forward
+ * pass' first product), 7 up to 32 rows. */
 void lrcnn_debug_ffn_tile(int32_t tile);
 
 /* Byte offset in the layer-wise workspace of node `node`'s full feature map

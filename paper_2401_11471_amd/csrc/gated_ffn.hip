@@ -505,7 +505,7 @@ struct Wide {
   static constexpr int PART = 8192 + 8192 * RB;
   static constexpr int LDS = FB == 4 && 4 * PART > ST * STAGE ? 4 * PART : ST * STAGE;
 };
-template <typename T, typename W, int EPI>
+template <typename T, typename W, int EPI, bool DMA>
 __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(FfnArgs a) {
   constexpr int E = 16 / (int)sizeof(T), BK = kRow / (int)sizeof(T);
   constexpr int FB = W::FB, RB = W::RB, STAGE = W::STAGE, ST = W::ST;
@@ -544,10 +544,37 @@ __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(F
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem +
                         wave * 8 * kRow;
   int kpos = 0;  // of the step to copy
+  // Not aligned: a step's copy j is a load and, a step later, in the place where the
+  // next one's is issued, a write to LDS.
+  typedef std::conditional_t<sizeof(T) == 2, u32x4_a2, u32x4_a4> u32x4_a;
+  u32x4 held[DMA ? 1 : LD];
+  auto pull = [&](int j, auto whole) {
+    typedef __attribute__((address_space(1))) const char g_char;
+    g_char *p = (g_char *)(j < LF ? gw : gx) + off[j];
+    const int n = a.depth - kpos - vec * E;
+    if (decltype(whole)::value || n >= E) {
+      held[j] = *(__attribute__((address_space(1))) const u32x4_a *)p;
+    } else {
+      uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (e < n) {
+          const T v = ((__attribute__((address_space(1))) const T *)p)[e];
+          if constexpr (sizeof(T) == 2) w[e / 2] |= (uint32_t)v << (16 * (e & 1));
+          else w[e] = __float_as_uint(v);
+        }
+      held[j] = (u32x4){w[0], w[1], w[2], w[3]};
+    }
+  };
+  typedef __attribute__((address_space(3))) u32x4 lds_vec;
+  lds_char *const mine = (lds_char *)smem + br * kRow + (tid & 7) * 16;
   // WHOLE: the step's depth is there to its end
   auto bring = [&](int st, int j, auto whole) {
     const uint32_t to = lds0 + st * STAGE + 32 * kRow * j;
-    if constexpr (decltype(whole)::value) {
+    if constexpr (!DMA) {
+      *(lds_vec *)(mine + st * STAGE + 32 * kRow * j) = held[j];
+      pull(j, whole);
+    } else if constexpr (decltype(whole)::value) {
       copy16(j < LF ? gw : gx, off[j], to);
     } else {
       const bool ok = kpos + vec * E < a.depth;
@@ -625,7 +652,7 @@ __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(F
       constexpr int C = LAST ? 0 : LD, C2 = 3 * C / 8, C3 = (C - C2) / 2 + C2;
       __syncthreads();
       slice(I(2), I(0), I(0), nx, I(0), I(C2), st, whole);
-      wait_vmcnt<C2>();
+      if constexpr (DMA) wait_vmcnt<C2>();
       __syncthreads();
       slice(I(3), I(0), I(LAST ? 0 : 1), nx, I(C2), I(C3), st, whole);
       if constexpr (!LAST) {
@@ -634,7 +661,7 @@ __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(F
       }
     } else {
       constexpr int C = LAST ? 0 : LD, R1 = LAST ? 0 : 1;
-      wait_vmcnt<(ST - 2) * LD>();
+      if constexpr (DMA) wait_vmcnt<(ST - 2) * LD>();
       __syncthreads();
       slice(I(2), I(0), I(R1), nx, I(0), I(C / 4), st, whole);
       slice(I(3), I(1), I(R1), nx, I(C / 4), I(C / 2), st, whole);
@@ -647,12 +674,18 @@ __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(F
     st = nx;
   };
   using std::false_type;
+  if constexpr (!DMA) {
+#pragma unroll
+    for (int j = 0; j < LD; ++j) pull(j, false_type());
+    advance();
+  }
+#pragma unroll 1
   for (int i = 0; i < ST; ++i) {
 #pragma unroll
     for (int j = 0; j < LD; ++j) bring(i, j, false_type());
     advance();
   }
-  wait_vmcnt<(ST - 1) * LD>();
+  if constexpr (DMA) wait_vmcnt<(ST - 1) * LD>();
   __syncthreads();
   each<0, N>([&](auto k) { fragment(0, I(0), k); });
   if constexpr (ST == 2) {
@@ -668,7 +701,7 @@ __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(F
   for (; t + 1 < steps; ++t) turn(false_type(), false_type());
   turn(false_type(), std::true_type());
 #undef I
-  wait_vmcnt<0>();
+  if constexpr (DMA) wait_vmcnt<0>();
   const int wrow = r0 + wr * 32 * RB;
   __syncthreads();
   if constexpr (!CODES) {
@@ -887,7 +920,6 @@ typedef Wide<4, 4, 2> Big;                // 256 features x 256 rows
 typedef Wide<4, 2, 3> Half;               // 256 x 128
 typedef Wide<2, 2, 2> Mid;                // 128 x 128
 typedef Wide<2, 2, 4> Deep;            // 128 x 128, one workgroup a CU
-typedef Tile<2, 2, 2, 2, 1, 2> Plain;  // 128 x 128 of operands that are not aligned
 typedef Tile<1, 2, 1, 2, 4, 3> Small;  // 64 x 64, 4 waves that split the depth
 typedef Tile<1, 2, 1, 1, 4, 3> Tiny;   // 64 x 32
 typedef Tile<1, 1, 1, 1, 4, 3> Least;  // 32 x 32, one block of features
@@ -908,10 +940,10 @@ int launch(FfnArgs &a, hipStream_t s) {
   return LRCNN_OK;
 }
 
-template <typename T, typename W, int EPI>
+template <typename T, typename W, int EPI, bool DMA>
 int launch_wide(FfnArgs &a, hipStream_t s) {
   lay_out(a, W::R, EPI == EPI_GATE ? W::F / 2 : W::F);
-  ffn_wide_kernel<T, W, EPI><<<(unsigned)(a.gx * a.gy), 256, 0, s>>>(a);
+  ffn_wide_kernel<T, W, EPI, DMA><<<(unsigned)(a.gx * a.gy), 256, 0, s>>>(a);
   return LRCNN_OK;
 }
 
@@ -920,7 +952,7 @@ std::atomic<int> g_tile{-1};  // test hook: the variant to take where it can
 template <typename T, int EPI>
 int product(FfnArgs a, hipStream_t s) {
   constexpr int H = EPI == EPI_GATE ? 2 : 1;
-  constexpr int kFew = 8;  // number of the variant for few rows; the others: costs below
+  constexpr int kFew = 7;  // number of the variant for few rows; the others: costs below
   const int forced = g_tile;
   if (a.rows <= kFewRows && (forced < 0 || forced == kFew)) {
     auto few = [&](auto nc, auto nf) {
@@ -951,31 +983,31 @@ int product(FfnArgs a, hipStream_t s) {
   constexpr int G = EPI == EPI_GATE ? 0 : EPI == EPI_BACK ? 1 : 2;
   struct Cost {
     int f, r, alone, busy, finish[3];
-    bool wide, plain;
+    bool wide;
   };
   constexpr Cost costs[] = {
-      {Big::F, Big::R, F32 ? 7100 : 1100, F32 ? 7100 : 1150, {20000, 40000, 6000}, true, false},
-      {Half::F, Half::R, F32 ? 3600 : 800, F32 ? 3600 : 900, {9000, 18000, 3000}, true, false},
-      {Mid::F, Mid::R, F32 ? 1850 : 620, F32 ? 1850 : 530, {1500, 5000, 1500}, true, false},
-      {Deep::F, Deep::R, F32 ? 1850 : 550, F32 ? 1850 : 550, {6000, 10000, 3000}, true, false},
-      {Plain::F, Plain::R, F32 ? 2100 : 600, F32 ? 2100 : 700, {1500, 5000, 1500}, false, true},
-      {Small::F, Small::R, F32 ? 690 : 290, F32 ? 630 : 220, {2200, 4000, 1000}, false, false},
-      {Tiny::F, Tiny::R, F32 ? 440 : 220, F32 ? 370 : 160, {1400, 2500, 700}, false, false},
-      {Least::F, Least::R, F32 ? 300 : 170, F32 ? 190 : 100, {0, 1300, 400}, false, false}};
+      {Big::F, Big::R, F32 ? 7100 : 1100, F32 ? 7100 : 1150, {20000, 40000, 6000}, true},
+      {Half::F, Half::R, F32 ? 3600 : 800, F32 ? 3600 : 900, {9000, 18000, 3000}, true},
+      {Mid::F, Mid::R, F32 ? 1850 : 620, F32 ? 1850 : 530, {1500, 5000, 1500}, true},
+      {Deep::F, Deep::R, F32 ? 1850 : 550, F32 ? 1850 : 550, {6000, 10000, 3000}, true},
+      {Small::F, Small::R, F32 ? 690 : 290, F32 ? 630 : 220, {2200, 4000, 1000}, false},
+      {Tiny::F, Tiny::R, F32 ? 440 : 220, F32 ? 370 : 160, {1400, 2500, 700}, false},
+      {Least::F, Least::R, F32 ? 300 : 170, F32 ? 190 : 100, {0, 1300, 400}, false}};
   const int64_t steps = ((int64_t)a.depth * (int64_t)sizeof(T) + kRow - 1) / kRow;
   int pick = -1;
   int64_t least_time = 0;
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < 7; ++i) {
     const Cost &c = costs[i];
-    if ((c.wide && !(dma && near)) || (c.plain && dma && near && forced != i)) continue;
-    if ((i == 7 && EPI == EPI_GATE) || tiles(c.f, c.r) > kMostTiles) continue;
+    // (half-sized tiles through registers are not built: never the best by a tenth)
+    if (c.wide && (!near || (!dma && i == 1))) continue;
+    if ((i == 6 && EPI == EPI_GATE) || tiles(c.f, c.r) > kMostTiles) continue;
     if (forced == i) {
       pick = i;
       break;
     }
     const int64_t n = (tiles(c.f, c.r) + 255) / 256;
     // (through registers, smaller tiles take half as long again)
-    const int64_t step = std::max<int64_t>(c.alone, n * c.busy) * (i > 4 && !dma ? 3 : 2) / 2;
+    const int64_t step = std::max<int64_t>(c.alone, n * c.busy) * (i > 3 && !dma ? 3 : 2) / 2;
     const int64_t time = steps * step + n * c.finish[G];
     if (pick < 0 || time < least_time) pick = i, least_time = time;
   }
@@ -983,14 +1015,17 @@ int product(FfnArgs a, hipStream_t s) {
     using TL = decltype(tile);
     return dma ? launch<T, TL, EPI, true>(a, s) : launch<T, TL, EPI, false>(a, s);
   };
+  auto wide = [&](auto tile) {
+    using W = decltype(tile);
+    return dma ? launch_wide<T, W, EPI, true>(a, s) : launch_wide<T, W, EPI, false>(a, s);
+  };
   switch (pick) {
-    case 0: return launch_wide<T, Big, EPI>(a, s);
-    case 1: return launch_wide<T, Half, EPI>(a, s);
-    case 2: return launch_wide<T, Mid, EPI>(a, s);
-    case 3: return launch_wide<T, Deep, EPI>(a, s);
-    case 4: return small(Plain());
-    case 5: return small(Small());
-    case 6: return small(Tiny());
+    case 0: return wide(Big());
+    case 1: return launch_wide<T, Half, EPI, true>(a, s);
+    case 2: return wide(Mid());
+    case 3: return wide(Deep());
+    case 4: return small(Small());
+    case 5: return small(Tiny());
   }
   if constexpr (EPI != EPI_GATE) return small(Least());
   return LRCNN_OK;

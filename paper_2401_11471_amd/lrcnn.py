@@ -734,7 +734,7 @@ def lrcnn_debug_fork_wgrad(mode):
 
 
 def lrcnn_debug_ffn_tile(tile):
-    """Test hook: the gated feed-forward block's tile (-1 by estimate; 0 .. 8 as the
+    """Test hook: the gated feed-forward block's tile (-1 by estimate; 0 .. 7 as the
     header lists them, where the operands allow it)."""
     LIB.lrcnn_debug_ffn_tile(tile)
 
