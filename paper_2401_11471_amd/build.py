@@ -12,7 +12,8 @@ LIB = os.path.join(HERE, "liblrcnn.so")
 SOURCES = ["plan.cpp", "exec.cpp", "kernels.hip", "conv_f32_fwd.hip", "conv_f32_dgrad.hip",
            "conv_bf16_fwd.hip", "conv_bf16_dgrad.hip", "wgrad.hip", "head.hip",
            "static_ws.hip", "act8.hip", "layer_norm.hip", "linear_wgrad.hip",
-           "group_norm.hip", "dropout.hip", "gated_ffn.hip"]
+           "group_norm.hip", "dropout.hip", "gated_ffn.hip", "gated_ffn_bf16.hip",
+           "gated_ffn_f32.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
