@@ -4,11 +4,18 @@
 //             where the caller wants them), z = a W2^T + b2
 //   backward  da = dz W2, du = da f'(u) v, dv = da f(u) (one kernel), dx = [du dv] W1
 //
-// All are products of rows with weights whose depth runs along both operands' rows.
-// The weights are the matrix instruction's first operand: a lane then holds
-// 16 of 32 neighbouring features of one row, its other half of the wave the other 16,
-// so that a checkpoint's group is 16 registers and one exchange between the halves, and
-// u and v of the same features are the same registers of two accumulators.
+// All are products of rows with weights whose depth runs along both operands' rows,
+// and differ in what becomes of a result. The weights are the matrix instruction's first
+// operand: a lane then holds runs of four neighbouring features of one row, and u and v of
+// the same features are the same registers of two accumulators.
+//
+// 67800 x 2048 x 8192 bf16: forward 4.14 ms for the first kernel with both checkpoints (4.55
+// TFLOP, 1100 TFLOP/s; the library's product of its size alone 3.25), 1.67 for the second
+// (1362 TFLOP/s; 1.58); backward 2.98 and 3.46 ms (the library's products 1.57 and 3.12).
+// The plain products keep the matrix pipes 78% busy at 1.62 GHz, the clock that their own
+// power leaves; the first forward kernel 57% at 1.68, the first backward one 37% at 1.93:
+// a tile's results take 20 and 42 us of vector instructions (a tile's products 37), which
+// one wave on a SIMD doesn't overlap with products.
 #pragma once
 
 #include "activation.hpp"
@@ -20,8 +27,6 @@
 
 namespace lrcnn {
 namespace act8 {
-// The products' entries, one translation unit for each storage type
-
 enum Epi {
   EPI_GATE,  // f(u) v, u and v
   EPI_BACK,  // du and dv from da
@@ -78,8 +83,9 @@ __device__ __forceinline__ void wave_meets() {
 // on of row lane % 32. They are read back eight features to a lane, a row's
 // lanes next to each other: whole cache lines to memory, a checkpoint's group in a quad of
 // lanes, and one copy of the code for all strips (unrolled over the accumulators it
-// is fetched anew for every tile and takes three times as long). 16-byte slots are
-// swapped by the row, so the lanes of a pass take different banks.
+// is fetched anew for every tile: with silu, without checkpoints, 22 us a tile of 256 x 256
+// beside its products, so 14). 16-byte slots are swapped by the row, so the lanes of a
+// pass take different banks.
 template <int FB>
 __device__ __forceinline__ lds_char *slot_of(lds_char *l, int row, int slot) {
   return l + (row * 8 * FB + (slot ^ (row & 7))) * 16;
@@ -931,10 +937,12 @@ __global__ __launch_bounds__(512) void ffn_few_kernel(FfnArgs a) {
 typedef Wide<4, 4, 2> Big;                // 256 features x 256 rows
 typedef Wide<4, 2, 3> Half;               // 256 x 128
 typedef Wide<2, 2, 2> Mid;                // 128 x 128
-typedef Wide<2, 2, 4> Deep;            // 128 x 128, one workgroup a CU
-typedef Tile<1, 2, 1, 2, 4, 3> Small;  // 64 x 64, 4 waves that split the depth
-typedef Tile<1, 2, 1, 1, 4, 3> Tiny;   // 64 x 32
-typedef Tile<1, 1, 1, 1, 4, 3> Least;  // 32 x 32, one block of features
+typedef Wide<2, 2, 4> Deep;               // 128 x 128, one workgroup a CU
+typedef Tile<1, 2, 1, 2, 4, 3> Small;     // 64 x 64, 4 waves that split the depth
+typedef Tile<1, 2, 1, 1, 4, 3> Tiny;      // 64 x 32
+typedef Tile<1, 1, 1, 1, 4, 3> Least;     // 32 x 32, one block of features
+// (32 rows, few and the best tile, us: z of 2048 x 8192 bf16 23 and 31, 2048 x 512 float32
+// 12.5 and 29; first kernel 18.2 and 14.6, 11.4 and 11.9)
 constexpr int kFewRows = 32;
 
 void lay_out(FfnArgs &a, int rows, int feats) {
@@ -986,7 +994,10 @@ int product(FfnArgs a, hipStream_t s) {
                     Big::R * a.x.ld * (int64_t)sizeof(T) < (int64_t)1 << 32;
   // The variant of the least estimated time: for n tiles on the busiest of 256 CUs,
   // steps * max(alone, n * busy) + n * finish, in ns measured with one tile on a CU, with
-  // many, and for the results.
+  // many, and for the results. (Measured by variant from 392 x 512 x 2048 to 67800 x 2048 x
+  // 8192, the pick is within a tenth of the best: 3136 x 1024 x 2736 bf16 in tiles of 256
+  // x 256, 256 x 128, 128 x 128 two and one a CU, 64 x 64, 64 x 32: first kernel 71, 63, 50,
+  // 64, 83, 85 us, z 56, 41, 32, 30, 47, 60; picked 50 and 29.)
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int G = EPI == EPI_GATE ? 0 : EPI == EPI_BACK ? 1 : 2;
   struct Cost {

@@ -6,13 +6,22 @@
 //             dx = rstd (q - mean(q) - xh mean(q xh)),
 //             dgamma = sum of e xh, dbeta = sum of e
 //
-// A group's sums need all its pixels before the first result, so a map is read
-// twice: a pass that leaves, for every channel of a slab of pixels, two numbers
-// (forward: mean and centred sum of squares; backward: sums of e and e xh), a small
-// kernel that joins them by group (and by channel for dgamma, dbeta), and a pass
-// that applies the result. A channel's two numbers serve every way of
+// A group's sums need all its pixels before the first result. A map whose groups fit
+// the registers of a block is read once, in one launch: 1 x 49 x 512 bf16 6.9 us, 7 x 169
+// x 510 float32 10.5 (three launches: 13.8 and 19.2), a chain of loads, two reductions and
+// a store each. Other maps are read twice: a pass that leaves, for every channel of a
+// slab of pixels, two numbers (forward: mean and centred sum of squares; backward: sums of e
+// and e xh), a small kernel that joins them by group (and by channel for dgamma, dbeta),
+// and a pass that applies the result. A channel's two numbers serve every way of
 // grouping, whatever the group's width and alignment, and in the backward pass both
 // the groups' means (weighted by gamma) and the parameters' gradients.
+//
+// Large maps are bound by HBM: 8 x 135000 x 512 bf16 with relu and checkpoint 235 us for the
+// sums (4.7 TB/s), 8 for the join, 532 for the result (5.2 TB/s); backward from the
+// checkpoint with silu, 8 x 8475 x 2048 bf16, 115 and 124 us (3.9 and 5.7 TB/s; the first
+// also by its vector instructions, 0.19 a cycle and SIMD). Small parts of a batch at a time,
+// so that the second pass finds the map in the Infinity Cache, took longer (1317 us and
+// 1078 with the unpack): what the pass before has written goes to memory meanwhile.
 //
 // Statistics: eight pixels at a time are centred in registers (their mean
 // corrected by the centred sum), then joined with
@@ -31,7 +40,10 @@ namespace {
 
 constexpr int64_t kMaxImages = 1 << 20, kMaxChannels = 1 << 20;
 constexpr int kBatch = 8;         // pixels that a thread holds at a time
-constexpr int kLeast = 2;         // pixels a thread, where the CUs have no work else
+// Pixels a thread, where the CUs have no work else (8 x 784 x 96 float32 backward: 8 pixels
+// 18.8 us, 2 pixels 14.6; but with blocks for all CUs a thread's constants for its channels
+// take as long as a few pixels: 25 x 185 x 2023 bf16 backward 76 and 64 us)
+constexpr int kLeast = 2;
 constexpr int kUnits = 2048;      // blocks of a pass, where there are as many
 constexpr int kApplyPixels = 4;   // applying passes: pixels in flight a thread
 
@@ -789,7 +801,8 @@ int64_t most_units(int64_t batch, int64_t cols) {
 
 // The block of a call whose groups fit into one: whole groups, at least 64 bytes of
 // a pixel, few idle lanes, where there is a checkpoint whole groups of 32 channels (or all
-// channels); pixels a thread R. width 0: they do not fit.
+// channels); two pixels a thread where there are as many threads (7 x 169 x 510 float32: one
+// 12.5 us, two 10.3), at most most_r, which the registers hold. width 0: they do not fit.
 struct Block {
   int width = 0, tpr = 0, threads = 0, r = 0;
 };
@@ -813,6 +826,7 @@ Block block_of(int64_t batch, int64_t pixels, int64_t cols, int64_t per, int es,
   const int64_t r = up(pixels, best.threads / best.tpr);
   best.r = r <= 1 ? 1 : r <= 2 ? 2 : r <= 4 ? 4 : 8;
   // few large blocks leave most of the CUs idle for longer than two more launches take
+  // (backward 8 x 784 x 96 float32, 32 blocks: 20.4 us, by slabs 14.6)
   if (batch * up(cols, best.width) < 128 && best.threads * best.r > 1024) best.width = 0;
   return best;
 }
