@@ -60,7 +60,6 @@ typedef uint32_t u32x4_a4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int kRow = 128;  // bytes of a tile's row in LDS: 64 bfloat16 or 32 float32 of depth
 
-
 // ------------------------------------------------------------- results
 // f(0), f(1), ... f(N - 1), the index a constant
 template <int B, int E, typename F>
@@ -232,21 +231,20 @@ __device__ __forceinline__ void tile_of(const FfnArgs &a, int *x, int *y) {
   *x = (int)(8 * p + tx), *y = (int)ty;
 }
 
-// A tile of WF FB blocks of 32 features by WR RB of 32 rows. KS waves split the depth
-// of each step among them and are summed at the end (1: WF x WR waves of FB x RB blocks each).
-// ST: LDS stages.
-template <int WF_, int FB_, int WR_, int RB_, int KS_, int ST_>
+// Small products: a tile of FB blocks of 32 features by RB of 32 rows. Its four waves
+// split the depth of each step, a quarter each, and are summed at the end; so 32 rows by 32
+// features are still work for a whole CU. ST: LDS stages.
+template <int FB_, int RB_, int ST_>
 struct Tile {
-  static constexpr int WF = WF_, FB = FB_, WR = WR_, RB = RB_, KS = KS_, ST = ST_;
-  static constexpr int F = 32 * WF * FB, R = 32 * WR * RB, THREADS = 64 * WF * WR * KS;
-  static constexpr int STAGE = (F + R) * kRow;
-  static constexpr int SUMS = KS > 1 ? KS * FB * RB * 64 * 16 * 4 : 0;
+  static constexpr int FB = FB_, RB = RB_, ST = ST_, KS = 4;
+  static constexpr int F = 32 * FB, R = 32 * RB, THREADS = 64 * KS;
+  static constexpr int STAGE = (F + R) * kRow, SUMS = KS * FB * RB * 64 * 16 * 4;
   static constexpr int LDS = ST * STAGE > SUMS ? ST * STAGE : SUMS;
-  static_assert(LDS >= THREADS / 64 * 32 * 32 * FB * 4, "a strip for each wave");
+  static_assert(LDS >= RB * 32 * 32 * FB * 4, "a strip for each wave that has rows");
 };
 
-// One step's products: fragments from an LDS stage. K order: lane half g takes the
-// 16-byte vectors 4 g + q of a tile row, q = 0 .. 3, of both operands alike.
+// A quarter of a step's products: fragments from an LDS stage. K order: lane half g takes
+// the 16-byte vectors 4 g + q of a tile row, q = 0 .. 3, of both operands alike.
 template <typename T, int FB, int RB>
 __device__ __forceinline__ void products(const char *wt, const char *xt, int q, int lane,
                                          f32x16 (&acc)[FB][RB]) {
@@ -356,17 +354,9 @@ __global__ __launch_bounds__(TL::THREADS) void ffn_kernel(FfnArgs a) {
     for (int j = 0; j < RB; ++j)
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
-  const int wk = KS > 1 ? wave : 0, wp = KS > 1 ? 0 : wave;
-  const int wf = wp % TL::WF, wr = wp / TL::WF;
   auto multiply = [&](int st) {
-    const char *wt = smem + st * TL::STAGE + wf * 32 * FB * kRow;
-    const char *xt = smem + st * TL::STAGE + (TL::F + wr * 32 * RB) * kRow;
-    if constexpr (KS > 1) {
-      products<T, FB, RB>(wt, xt, wk, lane, acc);
-    } else {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) products<T, FB, RB>(wt, xt, q, lane, acc);
-    }
+    const char *wt = smem + st * TL::STAGE;
+    products<T, FB, RB>(wt, wt + TL::F * kRow, wave, lane, acc);
   };
   if constexpr (DMA) {
     const void *zero = &g_zero16[0];
@@ -443,48 +433,40 @@ __global__ __launch_bounds__(TL::THREADS) void ffn_kernel(FfnArgs a) {
       if (t + 1 < steps) step(t + 1, reg0);
     }
   }
-  const int c0 = f0 + wf * Lanes<EPI, FB>::WIDTH;
   Bias bias;
-  bias.load<EPI>(a, c0 + 8 * (lane % Lanes<EPI, FB>::PER));
+  const int c = f0 + 8 * (lane % Lanes<EPI, FB>::PER);
+  bias.load<EPI>(a, c);
   __syncthreads();
-  if constexpr (KS > 1) {
-    // the waves' sums joined in order; wave j takes the blocks of rows j
-    float *red = (float *)smem;
+  // the waves' sums joined in order; wave j takes the blocks of rows j
+  float *red = (float *)smem;
+#pragma unroll
+  for (int i = 0; i < FB; ++i)
+#pragma unroll
+    for (int j = 0; j < RB; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        red[(((wave * FB + i) * RB + j) * 16 + v) * 64 + lane] = acc[i][j][v];
+  __syncthreads();
+  if (wave < RB) {
 #pragma unroll
     for (int i = 0; i < FB; ++i)
 #pragma unroll
-      for (int j = 0; j < RB; ++j)
+      for (int v = 0; v < 16; ++v) {
+        float s = 0.f;
 #pragma unroll
-        for (int v = 0; v < 16; ++v)
-          red[(((wk * FB + i) * RB + j) * 16 + v) * 64 + lane] = acc[i][j][v];
-    __syncthreads();
-    if (wave < RB) {
-#pragma unroll
-      for (int i = 0; i < FB; ++i)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          float s = 0.f;
-#pragma unroll
-          for (int k = 0; k < KS; ++k) s += red[(((k * FB + i) * RB + wave) * 16 + v) * 64 + lane];
-          acc[i][0][v] = s;
-        }
-    }
-    __syncthreads();
-    if (wave >= RB) return;
+        for (int k = 0; k < KS; ++k) s += red[(((k * FB + i) * RB + wave) * 16 + v) * 64 + lane];
+        acc[i][0][v] = s;
+      }
   }
+  __syncthreads();
+  if (wave >= RB) return;
   lds_char *const strip = (lds_char *)smem + wave * 32 * 32 * FB * 4;
-#pragma unroll 1
-  for (int j = 0; j < (KS > 1 ? 1 : RB); ++j) {
-    each<0, KS == 1 ? RB : 1>([&](auto j_) {
-      if (j == j_) each<0, FB>([&](auto i) { strip_put<FB>(strip, i, acc[i][j_]); });
-    });
-    wave_meets();
-    const int rj = r0 + 32 * (KS > 1 ? wave : wr * RB + j);
-    strip_rows<T, EPI, FB>(a, strip, rj, c0, bias, [&](int row, float (&u)[8], float (&v)[8]) {
-      read_uv<T>(a, rj + row, c0 + 8 * (lane % Lanes<EPI, FB>::PER), u, v);
-    });
-    wave_meets();
-  }
+  each<0, FB>([&](auto i) { strip_put<FB>(strip, i, acc[i][0]); });
+  wave_meets();
+  const int rj = r0 + 32 * wave;
+  strip_rows<T, EPI, FB>(a, strip, rj, f0, bias, [&](int row, float (&u)[8], float (&v)[8]) {
+    read_uv<T>(a, rj + row, c, u, v);
+  });
 }
 
 // Large products: four waves of FB x RB blocks of 32 x 32, one on each matrix pipe, two by
@@ -938,9 +920,9 @@ typedef Wide<4, 4, 2> Big;                // 256 features x 256 rows
 typedef Wide<4, 2, 3> Half;               // 256 x 128
 typedef Wide<2, 2, 2> Mid;                // 128 x 128
 typedef Wide<2, 2, 4> Deep;               // 128 x 128, one workgroup a CU
-typedef Tile<1, 2, 1, 2, 4, 3> Small;     // 64 x 64, 4 waves that split the depth
-typedef Tile<1, 2, 1, 1, 4, 3> Tiny;      // 64 x 32
-typedef Tile<1, 1, 1, 1, 4, 3> Least;     // 32 x 32, one block of features
+typedef Tile<2, 2, 3> Small;              // 64 x 64
+typedef Tile<2, 1, 3> Tiny;               // 64 x 32
+typedef Tile<1, 1, 3> Least;              // 32 x 32, one block of features
 // (32 rows, few and the best tile, us: z of 2048 x 8192 bf16 23 and 31, 2048 x 512 float32
 // 12.5 and 29; first kernel 18.2 and 14.6, 11.4 and 11.9)
 constexpr int kFewRows = 32;
