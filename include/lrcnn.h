@@ -551,8 +551,8 @@ int lrcnn_dropout(int64_t rows, int64_t cols, int32_t dtype, const void *x,
  * float32 [n_out], nullable. z may be NULL (w2 and b2 are not read then, n_out is
  * ignored). For the backward pass, each nullable: uv [rows][2 hidden] receives u
  * and v; ckpt_u, ckpt_v the checkpoints of their float32 values.
- * ESHAPE beyond 2^24 features, 2^30 rows or 2^22 tiles of 128 x 128 of a
- * product's result. */
+ * ESHAPE beyond 2^24 features or 2^30 rows, and from 2^22 tiles of 128 x 128 of
+ * a product's result on. */
 int lrcnn_gated_ffn_forward(int64_t rows, int64_t n_in, int64_t hidden,
                             int64_t n_out, int32_t dtype, int32_t kind,
                             const void *x, int64_t ldx, const void *w1,

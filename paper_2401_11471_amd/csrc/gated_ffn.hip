@@ -23,8 +23,8 @@ int ffn_shape(int64_t rows, int64_t n, int64_t hidden, int32_t dtype, int32_t ki
   if (hidden < 1) return refuse(LRCNN_ESHAPE, "need hidden >= 1");
   if (n > kMaxFeatures || hidden > kMaxFeatures / 2 || rows > kMaxFfnRows)
     return refuse(LRCNN_ESHAPE, "gated_ffn takes at most 2^24 features and 2^30 rows");
-  if (((rows + 127) / 128) * ((std::max(n, 2 * hidden) + 127) / 128) > kMostTiles)
-    return refuse(LRCNN_ESHAPE, "gated_ffn takes at most 2^22 tiles of 128 x 128");
+  if (((rows + 127) / 128) * ((std::max(n, 2 * hidden) + 127) / 128) > kMostMidTiles)
+    return refuse(LRCNN_ESHAPE, "gated_ffn takes fewer than 2^22 tiles of 128 x 128");
   if (kind < LRCNN_ACT_RELU || kind > LRCNN_ACT_SILU)
     return refuse(LRCNN_EINVAL, "unknown activation");
   return LRCNN_OK;

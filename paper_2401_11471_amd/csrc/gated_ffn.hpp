@@ -50,7 +50,9 @@ int ffn_bf16(Epi epi, const FfnArgs &a, hipStream_t s);
 int ffn_f32(Epi epi, const FfnArgs &a, hipStream_t s);
 extern std::atomic<int> g_ffn_tile;  // test hook: the variant to take where it can
 constexpr int64_t kMaxFeatures = 1 << 24, kMaxFfnRows = 1 << 30;
-constexpr int64_t kMostTiles = 1 << 22;  // tiles that a grid takes (2^32 threads)
+// Tiles that a grid takes: fewer than 2^32 threads, 256 a tile. Calls have fewer than 2^22
+// tiles of 128 x 128, so 64 x 64 ones, which take all operands, always fit.
+constexpr int64_t kMostTiles = (1 << 24) - 1, kMostMidTiles = (1 << 22) - 1;
 
 #ifdef LRCNN_FFN_KERNELS
 namespace {

@@ -141,6 +141,14 @@ def test_gated_ffn_refuses(call):
         assert call(kind=kind) == EINVAL
 
 
+@pytest.mark.parametrize("call,first", [(ffn_fwd, "x"), (ffn_bwd, "dz")])
+def test_gated_ffn_of_the_most_tiles(call, first):
+    """A tile of 64 x 64 has to be possible (fewer than 2^32 threads) wherever 128 x 128 is."""
+    most = dict(n_in=8, n_out=8, hidden=64)  # 128 features, a row of tiles 128 wide
+    assert call(rows=1 << 29, **most) == ESHAPE
+    assert call(rows=(1 << 29) - 128, **most, **{first: None}) == EINVAL
+
+
 def test_gated_ffn_forward_refuses():
     for k in ("x", "w1", "a", "w2"):
         assert ffn_fwd(**{k: None}) == EINVAL, k

@@ -326,6 +326,27 @@ def test_past_32_bits():
         assert torch.equal(p, q)
 
 
+def test_far_weights_in_many_tiles():
+    """Weights of 4 GiB, past the wide tiles' offsets, and more than 2^22 tiles of 64 x 64."""
+    rows, n_in, hidden = 1030, 128, 1 << 23
+    tell("gated far weights")
+    g = torch.Generator("cuda").manual_seed(11)
+    x = torch.randn(rows, n_in, device="cuda", generator=g).bfloat16()
+    w = torch.empty(2 * hidden, n_in, device="cuda", dtype=BF16).normal_(0, 0.3, generator=g)
+    a = torch.full((rows, hidden), math.nan, device="cuda", dtype=BF16)
+    L.lrcnn_gated_ffn_forward(L.ACT_SILU, x, w, a)
+    r = torch.cat([torch.randint(rows, (4000,), generator=g, device="cuda"),
+                   torch.tensor([0, rows - 1], device="cuda").repeat(2)])
+    f = torch.cat([torch.randint(hidden, (4000,), generator=g, device="cuda"),
+                   torch.tensor([0, 0, hidden - 1, hidden - 1], device="cuda")])
+    X, wu, wv = x[r].double(), w[f].double(), w[f + hidden].double()
+    u, v = (X * wu).sum(1), (X * wv).sum(1)
+    eu, ev = ((n_in + 8) * U * (X * t).abs().sum(1) for t in (wu, wv))
+    fu, _ = act(u, "silu")
+    error = (1.2 * eu + 4e-6 * u.abs()) * (v.abs() + ev) + fu.abs() * ev
+    assert ((a[r, f].double() - fu * v).abs() <= 2.0 ** -8 * (fu * v).abs() + 1.01 * error).all()
+
+
 @TYPES
 def test_in_a_graph_and_on_a_stream(dtype):
     """A captured forward and backward pass, on another stream than the tensors' own;
