@@ -550,7 +550,8 @@ int lrcnn_dropout(int64_t rows, int64_t cols, int32_t dtype, const void *x,
  * [n_out][hidden]; both dense, of the matrices' type. b1 float32 [2 hidden], b2
  * float32 [n_out], nullable. z may be NULL (w2 and b2 are not read then, n_out is
  * ignored). For the backward pass, each nullable: uv [rows][2 hidden] receives u
- * and v; ckpt_u, ckpt_v the checkpoints of their float32 values.
+ * and v; ckpt_u, ckpt_v the checkpoints of their float32 values. In place: z may
+ * be x; a and uv may not, nor z a: EINVAL.
  * ESHAPE beyond 2^24 features or 2^30 rows, and from 2^22 tiles of 128 x 128 of
  * a product's result on. */
 int lrcnn_gated_ffn_forward(int64_t rows, int64_t n_in, int64_t hidden,
@@ -569,7 +570,8 @@ int lrcnn_gated_ffn_forward(int64_t rows, int64_t n_in, int64_t hidden,
  * receives du and dv; ckpt_a (nullable) the checkpoint of f(u) * v; dx (NULL: not
  * wanted, w1t is not read then, n_in is ignored). The weights' gradients are
  * lrcnn_linear_wgrad's: of w2 from dz and ckpt_a, of w1 from duv and the
- * checkpoint of x. ESHAPE as in the forward pass. */
+ * checkpoint of x. In place: duv may be uv, dx may be dz or uv (not where that is
+ * duv); duv may not be dz: EINVAL. ESHAPE as in the forward pass. */
 int lrcnn_gated_ffn_backward(int64_t rows, int64_t n_in, int64_t hidden,
                              int64_t n_out, int32_t dtype, int32_t kind,
                              const void *dz, int64_t lddz, const void *w2t,

@@ -2,6 +2,7 @@
 #include "gated_ffn.hpp"
 
 #include <algorithm>
+#include <initializer_list>
 
 namespace lrcnn {
 namespace act8 {
@@ -27,6 +28,15 @@ int ffn_shape(int64_t rows, int64_t n, int64_t hidden, int32_t dtype, int32_t ki
     return refuse(LRCNN_ESHAPE, "gated_ffn takes fewer than 2^22 tiles of 128 x 128");
   if (kind < LRCNN_ACT_RELU || kind > LRCNN_ACT_SILU)
     return refuse(LRCNN_EINVAL, "unknown activation");
+  return LRCNN_OK;
+}
+
+// A product reads all of its inputs for each part of its result: what it writes has to
+// be other memory.
+int apart(const char *what, const void *out, std::initializer_list<const void *> in) {
+  if (out)
+    for (const void *p : in)
+      if (p == out) return refuse(LRCNN_EINVAL, what, " is an input of its product");
   return LRCNN_OK;
 }
 
@@ -67,6 +77,9 @@ extern "C" int lrcnn_gated_ffn_forward(int64_t rows, int64_t n_in, int64_t hidde
     TRY(take_f32("b2", b2, false));
     TRY(take("z", z, ldz, n_out, es, true, &zm));
   }
+  TRY(apart("a", a, {x, w1, b1, z ? w2 : nullptr, z ? (const void *)b2 : nullptr}));
+  TRY(apart("uv", uv, {x, w1, b1, a}));
+  if (z) TRY(apart("z", z, {a, w2, b2}));
   g.rows = (int)rows, g.depth = (int)n_in, g.feats = (int)hidden, g.kind = kind;
   g.w = w.p, g.bias = b1;
   g.ku = ckpt_of(ckpt_u, rows, hidden);
@@ -106,6 +119,8 @@ extern "C" int lrcnn_gated_ffn_backward(int64_t rows, int64_t n_in, int64_t hidd
     TRY(take("w1t", w1t, 0, 2 * hidden, es, true, &w1m));
     TRY(take("dx", dx, lddx, n_in, es, true, &xm));
   }
+  TRY(apart("duv", duv, {dz, w2t, dx ? w1t : nullptr}));
+  if (dx) TRY(apart("dx", dx, {duv, w1t}));
   g.rows = (int)rows, g.depth = (int)n_out, g.feats = (int)hidden, g.kind = kind;
   g.w = w.p;
   g.ku = ckpt_of(ckpt_u, rows, hidden);

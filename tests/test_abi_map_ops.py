@@ -278,3 +278,20 @@ def test_binding_refuses_tensors_of_another_gpu(stream, monkeypatch):
         monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
         run()
         assert calls.pop() == (101 if stream is None else stream) and not calls
+
+
+def test_gated_ffn_refuses_outputs_that_its_products_read():
+    """A product reads all rows and columns of its input while it writes its result."""
+    at = {k: P + 64 * (i + 1) for i, k in enumerate(("x", "w1", "b1", "a", "w2", "b2", "z"))}
+    for out, ins in (("a", ("x", "w1", "b1", "w2", "b2")), ("z", ("a", "w2", "b2"))):
+        for k in ins:
+            assert ffn_fwd(**{**at, out: at[k]}) == EINVAL, (out, k)
+            assert f"{out} is an input of its product" in last()
+    for k in ("x", "w1", "b1", "a"):
+        assert ffn_fwd(**at, uv=at[k]) == EINVAL, k
+        assert "uv is an input of its product" in last()
+    at = {k: P + 64 * (i + 1) for i, k in enumerate(("dz", "w2t", "uv", "duv", "w1t", "dx"))}
+    for out, ins in (("duv", ("dz", "w2t", "w1t")), ("dx", ("duv", "w1t"))):
+        for k in ins:
+            assert ffn_bwd(**{**at, out: at[k]}) == EINVAL, (out, k)
+            assert f"{out} is an input of its product" in last()

@@ -294,6 +294,41 @@ def test_by_differences(dtype):
     assert worst < top * (5e-3 if dtype == F32 else 3e-2)
 
 
+@TYPES
+@pytest.mark.parametrize("rows", [5, 33, 300, 2100])
+def test_in_place(rows, dtype):
+    """z over x, duv over uv, dx over dz, or over uv where duv is elsewhere; the
+    checkpoint of a over u's: the same as apart."""
+    tell("gated in place", rows, dtype)
+    n = 264
+    _, s = case(rows, n, n // 2, n, dtype, 12)
+    x, w2t, w1t = s["x"].to(dtype), s["w2"].t().contiguous(), s["w1"].t().contiguous()
+    a, uv = (torch.empty(rows, w, device="cuda", dtype=dtype) for w in (n // 2, n))
+    ku, kv, ka = (buf(rows, n // 2) for _ in range(3))
+    z, duv, dx = torch.empty_like(x), torch.empty_like(uv), torch.empty_like(x)
+    weights = s["w1"], a, s["b1"], s["w2"], s["b2"]
+    L.lrcnn_gated_ffn_forward(L.ACT_SILU, x, *weights, z, uv, ku, kv)
+    t = x.clone()
+    L.lrcnn_gated_ffn_forward(L.ACT_SILU, t, *weights, t)
+    assert torch.equal(t, z)
+    for held in (dict(ckpt_u=ku, ckpt_v=kv), dict(uv=uv)):
+        L.lrcnn_gated_ffn_backward(L.ACT_SILU, x, w2t, duv, ckpt_a=ka, w1t=w1t, dx=dx, **held)
+        t, o = x.clone(), torch.empty_like(duv)
+        mine = {k: v.clone() for k, v in held.items()}
+        if "uv" in held:
+            o = mine["uv"]
+            k = torch.empty_like(ka)
+        else:
+            k = mine["ckpt_u"]
+        L.lrcnn_gated_ffn_backward(L.ACT_SILU, t, w2t, o, ckpt_a=k, w1t=w1t, dx=t, **mine)
+        assert torch.equal(t, dx) and torch.equal(o, duv)
+        g = (n // 2 + 31) // 32 * 32 * rows
+        assert torch.equal(k[:g], ka[:g])
+    mine = uv.clone()
+    L.lrcnn_gated_ffn_backward(L.ACT_SILU, x, w2t, duv, mine, w1t=w1t, dx=mine)
+    assert torch.equal(mine, dx)
+
+
 def test_no_rows():
     x, w = torch.empty(0, 16, device="cuda"), torch.zeros(32, 16, device="cuda")
     k = torch.empty(0, device="cuda", dtype=torch.uint8)
