@@ -238,40 +238,46 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t m) {
 // group's exponent byte. All four lanes take part. Adding 1.5 2^23 rounds to
 // the nearest integer, ties to even, and leaves it in the low byte; the
 // product before it is exact, so one FMA does both.
-__device__ __forceinline__ uint2 encode8(const float (&v)[8], uint32_t *exponent) {
+__device__ __forceinline__ uint32_t largest_of(const float (&v)[8]) {
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-  m = quad_max(m);
-  uint32_t E = max((m + 0x10000u) >> 23, 7u);
-  uint2 q;
-  if (__builtin_expect(m >= 0x7f7f0000u, 0)) {
-    // the top binade's last step (the type's lowest value as a mask): held
-    // to +-127 steps of 2^121; infinity or NaN: the group stands for NaN
-    const bool bad = m >= 0x7f800000u;
-    E = bad ? 255u : 254u;
-    uint32_t w[2] = {0, 0};
+  return quad_max(m);
+}
+__device__ __forceinline__ uint32_t exponent_of(uint32_t m) { return max((m + 0x10000u) >> 23, 7u); }
+// below the top binade's last step
+__device__ __forceinline__ uint2 codes_of(const float (&v)[8], uint32_t E) {
+  const float inv = __uint_as_float((260u - E) << 23);
+  uint32_t b[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float s = fminf(fmaxf(v[i] * 0x1p-121f, -127.f), 127.f);
-      const uint32_t b = bad ? 0 : __float_as_uint(s + 12582912.f) & 0xffu;
-      w[i >> 2] |= b << (8 * (i & 3));
-    }
-    q = make_uint2(w[0], w[1]);
-  } else {
-    const float inv = __uint_as_float((260u - E) << 23);
-    uint32_t b[8];
+  for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(fmaf(v[i], inv, 12582912.f));
+  // low bytes of four words into one
+  const uint32_t lo0 = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u);
+  const uint32_t hi0 = __builtin_amdgcn_perm(b[3], b[2], 0x04000c0cu);
+  const uint32_t lo1 = __builtin_amdgcn_perm(b[5], b[4], 0x0c0c0400u);
+  const uint32_t hi1 = __builtin_amdgcn_perm(b[7], b[6], 0x04000c0cu);
+  return make_uint2(lo0 | hi0, lo1 | hi1);
+}
+// The top binade's last step (the type's lowest value as a mask): held to +-127
+// steps of 2^121; infinity or NaN: the group stands for NaN
+__device__ __forceinline__ bool at_top(uint32_t m) { return m >= 0x7f7f0000u; }
+__device__ __forceinline__ uint2 top_codes_of(const float (&v)[8], uint32_t m, uint32_t *E) {
+  const bool bad = m >= 0x7f800000u;
+  *E = bad ? 255u : 254u;
+  uint32_t w[2] = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(fmaf(v[i], inv, 12582912.f));
-    // low bytes of four words into one
-    const uint32_t lo0 = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u);
-    const uint32_t hi0 = __builtin_amdgcn_perm(b[3], b[2], 0x04000c0cu);
-    const uint32_t lo1 = __builtin_amdgcn_perm(b[5], b[4], 0x0c0c0400u);
-    const uint32_t hi1 = __builtin_amdgcn_perm(b[7], b[6], 0x04000c0cu);
-    q = make_uint2(lo0 | hi0, lo1 | hi1);
+  for (int i = 0; i < 8; ++i) {
+    const float s = fminf(fmaxf(v[i] * 0x1p-121f, -127.f), 127.f);
+    const uint32_t b = bad ? 0 : __float_as_uint(s + 12582912.f) & 0xffu;
+    w[i >> 2] |= b << (8 * (i & 3));
   }
-  *exponent = E;
-  return q;
+  return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ uint2 encode8(const float (&v)[8], uint32_t *exponent) {
+  const uint32_t m = largest_of(v);
+  *exponent = exponent_of(m);
+  if (__builtin_expect(at_top(m), 0)) return top_codes_of(v, m, exponent);
+  return codes_of(v, *exponent);
 }
 // 2^(E - 133) (NaN for E = 255); subnormal steps do not occur (E >= 7)
 __device__ __forceinline__ float step_of(uint32_t E) {
@@ -280,7 +286,7 @@ __device__ __forceinline__ float step_of(uint32_t E) {
 // Four codes times the step, exact
 __device__ __forceinline__ void decode4(uint32_t w, float step, float *v) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = (float)(int8_t)(w >> (8 * i)) * step;
+  for (int i = 0; i < 4; ++i) v[i] = (float)((int32_t)(w << (24 - 8 * i)) >> 24) * step;
 }
 __device__ __forceinline__ void decode8(uint2 q, uint32_t E, float (&v)[8]) {
   const float s = step_of(E);
