@@ -235,6 +235,55 @@ def test_every_tile(variant, dtype, tile):
     check_backward(rows, 77, 129, 65, dtype, "silu", 3, 1, True)
 
 
+@TYPES
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("variant", [0, 1])
+def test_whole_and_cut_strips(variant, kind, dtype, tile):
+    """Wide tiles with strips that are whole and that end early, rows and features, by kind."""
+    tile(variant)
+    for rows, n_in, hidden, n_out in [(300, 72, 200, 136), (260, 64, 256, 64)]:
+        check_forward(rows, n_in, hidden, n_out, dtype, kind, 8, 8, True, True)
+        check_backward(rows, n_in, hidden, n_out, dtype, kind, 8, 8, True)
+        check_backward(rows, n_in, hidden, n_out, dtype, kind, 8, 8, False)
+
+
+@pytest.mark.parametrize("variant", range(8))
+def test_groups_that_are_not_finite(variant, tile):
+    """A checkpoint's group that stands for NaN: its columns alone are spoiled, and the
+    checkpoint of a has NaN for the group; the type's largest values are held."""
+    tile(variant)
+    rows, n_in, hidden, n_out = (20 if variant == 7 else 300), 40, 200, 72
+    tell("groups", variant)
+    n, s = case(rows, n_in, hidden, n_out, F32, 6)
+    u, v, dz = n(rows, hidden), n(rows, hidden), n(rows, n_out)
+    w2t = s["w2"].t().contiguous()
+    results = []
+    for bad in (False, True):
+        if bad:
+            u[3, 70], v[5, 10] = math.nan, -math.inf
+            v[7, 130] = torch.finfo(F32).max
+        ku, kv, ka = (buf(rows, hidden) for _ in range(3))
+        L.lrcnn_act8_pack(u, ku)
+        L.lrcnn_act8_pack(v, kv)
+        duv = torch.empty(rows, 2 * hidden, device="cuda")
+        L.lrcnn_gated_ffn_backward(L.ACT_GELU, dz, w2t, duv, ckpt_u=ku, ckpt_v=kv, ckpt_a=ka)
+        results.append((duv, held(ka, rows, hidden), held(kv, rows, hidden)))
+    (good, ga, _), (got, a, hv) = results
+    spoiled = torch.zeros(rows, hidden, dtype=torch.bool, device="cuda")
+    spoiled[3, 64:96] = spoiled[5, :32] = spoiled[7, 128:160] = True
+    du, dv = got.chunk(2, 1)
+    assert torch.isnan(du[3, 64:96]).all() and torch.isnan(dv[3, 64:96]).all()
+    assert torch.isnan(du[5, :32]).all() and torch.isnan(a[5, :32]).all()
+    assert torch.equal(dv[5], good.chunk(2, 1)[1][5])      # dv has no v
+    assert torch.isnan(a[3, 64:96]).all()
+    assert hv[7, 130] == 127 * 2.0 ** 121                  # the top binade's last step
+    assert not torch.isnan(du[7]).any() and not torch.isnan(a[7]).any()
+    keep = ~spoiled
+    for p, q in zip((du, dv), good.chunk(2, 1)):
+        assert torch.equal(p[keep], q[keep])
+    assert torch.equal(a[keep], ga[keep])
+
+
 @pytest.mark.parametrize("variant", range(8))
 def test_rows_do_not_meet(variant, tile):
     """A row that is not finite spoils its own results alone, in every variant."""
