@@ -615,9 +615,13 @@ template <int FB_, int RB_, int ST_>
 struct Wide {
   static constexpr int FB = FB_, RB = RB_, F = 64 * FB, R = 64 * RB, STAGE = (F + R) * kRow;
   static constexpr int ST = ST_;
-  // EPI_BACK, 128 features a wave: a strip of 64 features and the codes of u and v
-  static constexpr int PART = 8192 + 8192 * RB;
-  static constexpr int LDS = FB == 4 && 4 * PART > ST * STAGE ? 4 * PART : ST * STAGE;
+  // EPI_BACK, 128 features a wave: a strip of 64 features and the codes of u and v, 8 KB
+  // for every 32 rows. The first rows' are behind the stages, if there is room.
+  static constexpr bool EARLY = ST * STAGE + 4 * 8192 <= 163840;
+  static constexpr int PART = 8192 + 8192 * (EARLY ? RB - 1 : RB);
+  static constexpr int LDS = FB < 4 ? ST * STAGE : EARLY ? ST * STAGE + 4 * 8192
+                             : ST * STAGE > 4 * PART ? ST * STAGE : 4 * PART;
+  static_assert(FB < 4 || 4 * PART <= (EARLY ? ST * STAGE : LDS), "a wave's part");
 };
 template <typename T, typename W, int EPI, bool DMA>
 __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(FfnArgs a) {
@@ -799,6 +803,42 @@ __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(F
     for (int j = 0; j < LD; ++j) bring(i, j, false_type());
     advance();
   }
+  // EPI_BACK from checkpoints: the codes of this wave's rows 32 j on, 1 KB a copy, and
+  // exponents of rows lane and lane + 64
+  const int wrow = r0 + wr * 32 * RB, wcol = f0 + wf * 128;
+  constexpr int HR = (RB + 1) / 2;
+  uint32_t eu[HR], ev[HR];
+  // (EARLY: a wave's part is the codes of j = 1 .. RB - 1, then the strip; else the strip first)
+  auto codes_at = [&](int j) {
+    return (lds_char *)smem + (W::EARLY && j == 0 ? ST * STAGE + wave * 8192
+                                                  : wave * W::PART + 8192 * (W::EARLY ? j - 1 : j + 1));
+  };
+  auto bring_codes = [&](int j) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = 32 * j + 8 * i + lane / 8, c = wcol + ((lane & 7) ^ (row & 7)) * 16;
+      const int64_t r = min(wrow + row, a.rows - 1);
+      const bool ok = c < a.ku.pitch;
+      const uint32_t to = (uint32_t)(uintptr_t)codes_at(j) + i * 1024;
+      const char *const zero = (const char *)&g_zero16[0];
+      copy16(ok ? (const char *)a.ku.q + r * a.ku.pitch + c : zero, to);
+      copy16(ok ? (const char *)a.kv.q + r * a.kv.pitch + c : zero, to + 4096);
+    }
+  };
+  const bool ck = CODES && a.ku.q && wcol < a.feats;
+  if constexpr (CODES) {
+#pragma unroll
+    for (int h = 0; h < HR; ++h) eu[h] = ev[h] = 0;
+    if (ck) {
+      if constexpr (W::EARLY) bring_codes(0);
+#pragma unroll
+      for (int h = 0; h < HR; ++h) {
+        const int64_t r = min(wrow + 64 * h + lane, a.rows - 1);
+        eu[h] = exponents4(a.ku, r, wcol);
+        ev[h] = exponents4(a.kv, r, wcol);
+      }
+    }
+  }
   if constexpr (DMA) wait_vmcnt<(ST - 1) * LD>();
   __syncthreads();
   each<0, N>([&](auto k) { fragment(0, I(0), k); });
@@ -815,8 +855,7 @@ __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(F
   for (; t + 1 < steps; ++t) turn(false_type(), false_type());
   turn(false_type(), std::true_type());
 #undef I
-  if constexpr (DMA) wait_vmcnt<0>();
-  const int wrow = r0 + wr * 32 * RB;
+  if constexpr (DMA || CODES) wait_vmcnt<0>();
   __syncthreads();
   if constexpr (!CODES) {
     const int c0 = f0 + wf * Lanes<EPI, FB>::WIDTH, k = lane % Lanes<EPI, FB>::PER;
@@ -850,37 +889,22 @@ __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(F
       wave_meets();
     }
   } else {
-    // This wave's LDS: a strip of 64 features, then the codes of u and v, 4 KB of
-    // each for 32 rows of 128 features. They are all on their way before the first
-    // store, as a wait for a load waits for the stores before it.
-    const int c0 = f0 + wf * 128;
-    lds_char *const strip = (lds_char *)smem + wave * W::PART, *const held = strip + 8192;
-    const bool ck = a.ku.q != nullptr, whole = wrow + 32 * RB <= a.rows && c0 + 128 <= a.feats;
-    constexpr int HR = (RB + 1) / 2;
-    uint32_t eu[HR], ev[HR];  // exponents of rows lane and lane + 64
-#pragma unroll
-    for (int h = 0; h < HR; ++h) eu[h] = ev[h] = 0;
-    if (ck && c0 < a.feats) {
-#pragma unroll 4
-      for (int i = 0; i < 4 * RB; ++i) {
-        const int row = 8 * i + lane / 8, c = c0 + ((lane & 7) ^ (row & 7)) * 16;
-        const int64_t r = min(wrow + row, a.rows - 1);
-        const bool ok = c < a.ku.pitch;
-        const uint32_t to = (uint32_t)(uintptr_t)held + (i / 4 * 8 + i % 4) * 1024;
-        const char *const zero = (const char *)&g_zero16[0];
-        copy16(ok ? (const char *)a.ku.q + r * a.ku.pitch + c : zero, to);
-        copy16(ok ? (const char *)a.kv.q + r * a.kv.pitch + c : zero, to + 4096);
-      }
-#pragma unroll
-      for (int h = 0; h < HR; ++h) {
-        const int64_t r = min(wrow + 64 * h + lane, a.rows - 1);
-        eu[h] = exponents4(a.ku, r, c0);
-        ev[h] = exponents4(a.kv, r, c0);
-      }
-      wait_vmcnt<0>();
+    // The first rows' codes are there; the others' are on their way while the strips of
+    // the first are worked on. (A wait for a load waits for the stores before it, so none
+    // is loaded later.)
+    lds_char *const strip = codes_at(W::EARLY ? RB : -1);
+    const bool whole = wrow + 32 * RB <= a.rows && wcol + 128 <= a.feats;
+    if (ck) {
+      for (int j = W::EARLY; j < RB; ++j) bring_codes(j);
+      if constexpr (!W::EARLY) wait_vmcnt<0>();
     }
 #pragma unroll 1
     for (int jh = 0; jh < 2 * RB; ++jh) {
+      if (W::EARLY && ck && jh == 2) {
+        // (two whole strips have at least 16 stores, newer than the codes)
+        if (whole) wait_vmcnt<16>();
+        else wait_vmcnt<0>();
+      }
       each<0, 2 * RB>([&](auto x) {
         constexpr int j = decltype(x)::value / 2, h = decltype(x)::value % 2;
         if (jh == x) {
@@ -891,22 +915,23 @@ __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(F
       wave_meets();
       const int j = jh >> 1, h = jh & 1, rj = wrow + 32 * j;
       const uint32_t wu = j < 2 ? eu[0] : eu[HR - 1], wv = j < 2 ? ev[0] : ev[HR - 1];
+      const lds_char *const held = codes_at(j);
       const int k = lane & 7;
       auto codes = [&](int row, float (&u)[8], float (&v)[8]) {
-        const int at = j * 8192 + row * 128 + ((4 * h + k / 2) ^ (row & 7)) * 16 + k % 2 * 8;
+        const int at = row * 128 + ((4 * h + k / 2) ^ (row & 7)) * 16 + k % 2 * 8;
         const int from = (32 * j + row) & 63, by = 8 * (2 * h + k / 4);
         decode8(lds_pair(held + at), (__shfl(wu, from) >> by) & 255u, u);
         decode8(lds_pair(held + at + 4096), (__shfl(wv, from) >> by) & 255u, v);
       };
       if (ck && whole) {
         with_kind(a.kind, [&](auto K) {
-          strip_whole<T, EPI, 2, decltype(K)::value>(a, strip, rj, c0 + 64 * h, Bias(), codes);
+          strip_whole<T, EPI, 2, decltype(K)::value>(a, strip, rj, wcol + 64 * h, Bias(), codes);
         });
       } else {
-        strip_rows<T, EPI, 2>(a, strip, rj, c0 + 64 * h, Bias(),
+        strip_rows<T, EPI, 2>(a, strip, rj, wcol + 64 * h, Bias(),
                               [&](int row, float (&u)[8], float (&v)[8]) {
                                 if (ck) codes(row, u, v);
-                                else read_uv<T>(a, rj + row, c0 + 64 * h + 8 * k, u, v);
+                                else read_uv<T>(a, rj + row, wcol + 64 * h + 8 * k, u, v);
                               });
       }
       wave_meets();
