@@ -244,7 +244,9 @@ __device__ __forceinline__ uint32_t largest_of(const float (&v)[8]) {
   for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
   return quad_max(m);
 }
-__device__ __forceinline__ uint32_t exponent_of(uint32_t m) { return max((m + 0x10000u) >> 23, 7u); }
+__device__ __forceinline__ uint32_t exponent_of(uint32_t m) {
+  return max((m + 0x10000u) >> 23, 7u);
+}
 // below the top binade's last step
 __device__ __forceinline__ uint2 codes_of(const float (&v)[8], uint32_t E) {
   const float inv = __uint_as_float((260u - E) << 23);

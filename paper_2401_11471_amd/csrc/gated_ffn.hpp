@@ -9,13 +9,13 @@
 // operand: a lane then holds runs of four neighbouring features of one row, and u and v of
 // the same features are the same registers of two accumulators.
 //
-// 67800 x 2048 x 8192 bf16: forward 4.14 ms for the first kernel with both checkpoints (4.55
-// TFLOP, 1100 TFLOP/s; the library's product of its size alone 3.25), 1.67 for the second
-// (1362 TFLOP/s; 1.58); backward 2.98 and 3.46 ms (the library's products 1.57 and 3.12).
+// 67800 x 2048 x 8192 bf16: forward 3.84 ms for the first kernel with both checkpoints (4.55
+// TFLOP, 1185 TFLOP/s; the library's product of its size alone 3.25), 1.70 for the second
+// (1340 TFLOP/s; 1.58); backward 2.60 and 3.42 ms (the library's products 1.57 and 3.12).
 // The plain products keep the matrix pipes 78% busy at 1.62 GHz, the clock that their own
-// power leaves; the first forward kernel 57% at 1.68, the first backward one 37% at 1.93:
-// a tile's results take 20 and 42 us of vector instructions (a tile's products 37), which
-// one wave on a SIMD doesn't overlap with products.
+// power leaves. In the first kernels a tile's results, which one wave on a SIMD
+// doesn't overlap with its products (37 us a tile), take 20 us forward and 39 backward;
+// their vector instructions are 8 and 17 of them.
 #pragma once
 
 #include "activation.hpp"
@@ -240,8 +240,8 @@ __device__ __forceinline__ void put_rows(const Ckpt &k, int64_t r, int step, int
       k.e[(r + i * step) * (k.pitch / kGroup) + c / kGroup] = (uint8_t)E[i];
   }
 }
-// As strip_rows where all of the strip's rows and features are there: its four passes
-// side by side, without branches between their instructions. The wave has a SIMD for
+// As strip_rows where all of the strip's rows and features are there: its passes side by
+// side, without branches between their instructions. The wave has a SIMD for
 // itself, and each pass is a chain of dependent ones (67800 x 2048 x 8192 bf16 with
 // checkpoints, one pass after another, two and four side by side: forward 4.14, 3.89, 3.85
 // ms, backward 2.98, 2.62, 2.62).
@@ -250,24 +250,18 @@ __device__ __forceinline__ void strip_whole(const FfnArgs &a, lds_char *l, int r
                                             const Bias &bias, Codes &&codes) {
   typedef Lanes<EPI, FB> N;
   constexpr int P = 32 / N::ROWS;
-  static_assert(P == 4, "passes of a strip");
   const int lane = threadIdx.x & 63, k = lane % N::PER, c = c0 + 8 * k, row = lane / N::PER;
   const int64_t r = r0 + row;
   float u[P][8], v[P][8], f[P][8], df[P][8];
+  if constexpr (EPI == EPI_GATE) {
 #pragma unroll
-  for (int j = 0; j < P; ++j) {
-    const int rj = row + j * N::ROWS;
-    if constexpr (EPI == EPI_GATE) {
-      const int slot = k / 4 * 16 + k % 4 * 2;
+    for (int j = 0; j < P; ++j) {
+      const int rj = row + j * N::ROWS, slot = k / 4 * 16 + k % 4 * 2;
       strip_get<FB>(l, rj, slot, u[j]);
       strip_get<FB>(l, rj, slot + 8, v[j]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) u[j][i] += bias.u[i], v[j][i] += bias.v[i];
-    } else {
-      codes(rj, u[j], v[j]);
     }
-  }
-  if constexpr (EPI == EPI_GATE) {
 #pragma unroll
     for (int j = 0; j < P; ++j)
 #pragma unroll
@@ -276,6 +270,7 @@ __device__ __forceinline__ void strip_whole(const FfnArgs &a, lds_char *l, int r
         f[j][i] *= v[j][i];
       }
   } else {
+    codes(row, u, v);
 #pragma unroll
     for (int j = 0; j < P; ++j) {
       float d[8];
@@ -328,6 +323,52 @@ __device__ __forceinline__ void read_uv(const FfnArgs &a, int64_t r, int c, floa
     get8(a.ku, r, c, u);
     get8(a.kv, r, c, v);
   }
+}
+
+// As read_uv, P rows `step` rows apart, all of them and the eight features there
+template <typename T, int P>
+__device__ __forceinline__ void read_whole(const FfnArgs &a, int64_t r, int step, int c,
+                                           float (&u)[P][8], float (&v)[P][8]) {
+  if (a.uv.p) {
+    Raw8<T> ru[P], rv[P];
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      const T *q = (const T *)a.uv.p + (r + j * step) * a.uv.ld + c;
+      ru[j] = load8(q, 8);
+      rv[j] = load8(q + a.feats, 8);
+    }
+#pragma unroll
+    for (int j = 0; j < P; ++j) ru[j].get(u[j]), rv[j].get(v[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      get8(a.ku, r + j * step, c, u[j]);
+      get8(a.kv, r + j * step, c, v[j]);
+    }
+  }
+}
+
+// A strip's results, EPI_BACK: with u and v from memory. whole: all of its rows and
+// features are there.
+template <typename T, int EPI, int FB, bool BESIDE>
+__device__ __forceinline__ void strip_out(const FfnArgs &a, lds_char *l, int r0, int c0,
+                                          const Bias &bias, bool whole) {
+  typedef Lanes<EPI, FB> N;
+  const int c = c0 + 8 * (threadIdx.x % 64 % N::PER);
+  if constexpr (BESIDE && EPI != EPI_PLAIN) {
+    if (whole) {
+      with_kind(a.kind, [&](auto K) {
+        strip_whole<T, EPI, FB, decltype(K)::value>(
+            a, l, r0, c0, bias, [&](int row, auto &u, auto &v) {
+              read_whole<T>(a, (int64_t)r0 + row, N::ROWS, c, u, v);
+            });
+      });
+      return;
+    }
+  }
+  strip_rows<T, EPI, FB>(a, l, r0, c0, bias, [&](int row, float (&u)[8], float (&v)[8]) {
+    read_uv<T>(a, r0 + row, c, u, v);
+  });
 }
 
 // ------------------------------------------------------------- products
@@ -578,9 +619,11 @@ __global__ __launch_bounds__(TL::THREADS) void ffn_kernel(FfnArgs a) {
   each<0, FB>([&](auto i) { strip_put<FB>(strip, i, acc[i][0]); });
   wave_meets();
   const int rj = r0 + 32 * wave;
-  strip_rows<T, EPI, FB>(a, strip, rj, f0, bias, [&](int row, float (&u)[8], float (&v)[8]) {
-    read_uv<T>(a, rj + row, c, u, v);
-  });
+  // (64 x 32, EPI_BACK: the registers of passes side by side cost it workgroups of the CU,
+  // 3136 x 1024 x 2736 bf16 59 -> 74 us; 64 x 64 59 -> 53)
+  constexpr bool BESIDE = !(EPI == EPI_BACK && FB > RB);
+  strip_out<T, EPI, FB, BESIDE>(a, strip, rj, f0, bias,
+                                rj + 32 <= a.rows && f0 + Lanes<EPI, FB>::WIDTH <= a.feats);
 }
 
 // Large products: four waves of FB x RB blocks of 32 x 32, one on each matrix pipe, two by
@@ -810,8 +853,8 @@ __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(F
   uint32_t eu[HR], ev[HR];
   // (EARLY: a wave's part is the codes of j = 1 .. RB - 1, then the strip; else the strip first)
   auto codes_at = [&](int j) {
-    return (lds_char *)smem + (W::EARLY && j == 0 ? ST * STAGE + wave * 8192
-                                                  : wave * W::PART + 8192 * (W::EARLY ? j - 1 : j + 1));
+    const int at = wave * W::PART + 8192 * (W::EARLY ? j - 1 : j + 1);
+    return (lds_char *)smem + (W::EARLY && j == 0 ? ST * STAGE + wave * 8192 : at);
   };
   auto bring_codes = [&](int j) {
 #pragma unroll
@@ -862,8 +905,7 @@ __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(F
     Bias bias;
     bias.load<EPI>(a, c0 + 8 * k);
     lds_char *const strip = (lds_char *)smem + wave * 32 * 32 * FB * 4;
-    const bool whole = EPI == EPI_GATE && FB == 4 && wrow + 32 * RB <= a.rows &&
-                       c0 + Lanes<EPI, FB>::WIDTH <= a.feats;
+    const bool whole = wrow + 32 * RB <= a.rows && c0 + Lanes<EPI, FB>::WIDTH <= a.feats;
 #pragma unroll 1
     for (int j = 0; j < RB; ++j) {
       each<0, RB>([&](auto j_) {
@@ -873,19 +915,7 @@ __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(F
         }
       });
       wave_meets();
-      const int rj = wrow + 32 * j;
-      if constexpr (EPI == EPI_GATE && FB == 4) {
-        if (whole) {
-          with_kind(a.kind, [&](auto K) {
-            strip_whole<T, EPI, FB, decltype(K)::value>(a, strip, rj, c0, bias, 0);
-          });
-          wave_meets();
-          continue;
-        }
-      }
-      strip_rows<T, EPI, FB>(a, strip, rj, c0, bias, [&](int row, float (&u)[8], float (&v)[8]) {
-        read_uv<T>(a, rj + row, c0 + 8 * k, u, v);
-      });
+      strip_out<T, EPI, FB, true>(a, strip, wrow + 32 * j, c0, bias, whole);
       wave_meets();
     }
   } else {
@@ -923,9 +953,17 @@ __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(F
         decode8(lds_pair(held + at), (__shfl(wu, from) >> by) & 255u, u);
         decode8(lds_pair(held + at + 4096), (__shfl(wv, from) >> by) & 255u, v);
       };
-      if (ck && whole) {
+      if (whole) {
+        auto all = [&](int row, auto &u, auto &v) {
+          if (ck) {
+#pragma unroll
+            for (int p = 0; p < 4; ++p) codes(row + 8 * p, u[p], v[p]);
+          } else {
+            read_whole<T>(a, (int64_t)rj + row, 8, wcol + 64 * h + 8 * k, u, v);
+          }
+        };
         with_kind(a.kind, [&](auto K) {
-          strip_whole<T, EPI, 2, decltype(K)::value>(a, strip, rj, wcol + 64 * h, Bias(), codes);
+          strip_whole<T, EPI, 2, decltype(K)::value>(a, strip, rj, wcol + 64 * h, Bias(), all);
         });
       } else {
         strip_rows<T, EPI, 2>(a, strip, rj, wcol + 64 * h, Bias(),
