@@ -12,10 +12,10 @@
 // 67800 x 2048 x 8192 bf16: forward 3.84 ms for the first kernel with both checkpoints (4.55
 // TFLOP, 1185 TFLOP/s; the library's product of its size alone 3.25), 1.70 for the second
 // (1340 TFLOP/s; 1.58); backward 2.60 and 3.42 ms (the library's products 1.57 and 3.12).
-// The plain products keep the matrix pipes 78% busy at 1.62 GHz, the clock that their own
-// power leaves. In the first kernels a tile's results, which one wave on a SIMD
-// doesn't overlap with its products (37 us a tile), take 20 us forward and 39 backward;
-// their vector instructions are 8 and 17 of them.
+// The plain products keep the matrix pipes 80% busy at 1.5 to 1.6 GHz, the clock that
+// their own power leaves; the first forward kernel 65% at 1.6, the first backward one 44% at
+// 1.9: of a tile's 57 and 76 us its results take 20 and 39, which one wave on a SIMD
+// doesn't overlap with products. Their vector instructions are 8 and 17 of them.
 #pragma once
 
 #include "activation.hpp"
