@@ -131,7 +131,7 @@ __device__ __forceinline__ void activate_all(int kind, const float (&u)[N], floa
                                              float (&df)[N]) {
   with_kind(kind, [&](auto K) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) activate<decltype(K)::value>(u[i], f[i], df[i]);
+    for (int i = 0; i < N; ++i) activate<decltype(K)::value, true>(u[i], f[i], df[i]);
   });
 }
 // A lane's eight features of a strip of FB blocks (EPI_GATE: blocks of u and v in turn)
@@ -266,7 +266,7 @@ __device__ __forceinline__ void strip_whole(const FfnArgs &a, lds_char *l, int r
     for (int j = 0; j < P; ++j)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        activate<KIND>(u[j][i], f[j][i], df[j][i]);
+        activate<KIND, true>(u[j][i], f[j][i], df[j][i]);
         f[j][i] *= v[j][i];
       }
   } else {
@@ -277,7 +277,7 @@ __device__ __forceinline__ void strip_whole(const FfnArgs &a, lds_char *l, int r
       strip_get<FB>(l, row + j * N::ROWS, 2 * k, d);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        activate<KIND>(u[j][i], f[j][i], df[j][i]);
+        activate<KIND, true>(u[j][i], f[j][i], df[j][i]);
         df[j][i] *= d[i] * v[j][i];
         d[i] *= f[j][i];
         f[j][i] *= v[j][i];
@@ -1177,8 +1177,8 @@ int product(FfnArgs a, hipStream_t s) {
   // steps * max(alone, n * busy) + n * finish, in ns measured with one tile on a CU, with
   // many, and for the results. (Measured by variant from 392 x 512 x 2048 to 67800 x 2048 x
   // 8192, the pick is within a tenth of the best: 3136 x 1024 x 2736 bf16 in tiles of 256
-  // x 256, 256 x 128, 128 x 128 two and one a CU, 64 x 64, 64 x 32: first kernel 71, 63, 50,
-  // 64, 83, 85 us, z 56, 41, 32, 30, 47, 60; picked 50 and 29.)
+  // x 256, 256 x 128, 128 x 128 two and one a CU, 64 x 64, 64 x 32: first kernel 64, 59, 51,
+  // 64, 86, 92 us, z 56, 40, 34, 30, 49, 60; picked 52 and 30.)
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int G = EPI == EPI_GATE ? 0 : EPI == EPI_BACK ? 1 : 2;
   struct Cost {
