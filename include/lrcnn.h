@@ -570,8 +570,9 @@ int lrcnn_gated_ffn_forward(int64_t rows, int64_t n_in, int64_t hidden,
  * receives du and dv; ckpt_a (nullable) the checkpoint of f(u) * v; dx (NULL: not
  * wanted, w1t is not read then, n_in is ignored). The weights' gradients are
  * lrcnn_linear_wgrad's: of w2 from dz and ckpt_a, of w1 from duv and the
- * checkpoint of x. In place: duv may be uv, dx may be dz or uv (not where that is
- * duv); duv may not be dz: EINVAL. ESHAPE as in the forward pass. */
+ * checkpoint of x. In place: duv may be uv (with uv's stride, else EINVAL), dx may be
+ * dz or uv (not where that is duv), ckpt_a may be ckpt_u or ckpt_v; duv may not be
+ * dz: EINVAL. ESHAPE as in the forward pass. */
 int lrcnn_gated_ffn_backward(int64_t rows, int64_t n_in, int64_t hidden,
                              int64_t n_out, int32_t dtype, int32_t kind,
                              const void *dz, int64_t lddz, const void *w2t,

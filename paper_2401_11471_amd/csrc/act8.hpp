@@ -92,6 +92,13 @@ inline int take(const char *what, const void *p, int64_t ld, int64_t cols, int e
   m->ld = ld ? ld : cols;
   return LRCNN_OK;
 }
+// An output in place of an input is that matrix: its rows are written where the same
+// rows are read, not where others still are.
+inline int same_rows(const char *what, const Mat &out, const Mat &in, int64_t rows) {
+  if (out.p && out.p == in.p && out.ld != in.ld && rows > 1)
+    return refuse(LRCNN_EINVAL, what, " is an input's memory with another row stride");
+  return LRCNN_OK;
+}
 inline int take_f32(const char *what, const void *p, bool must) {
   if (!p && must) return refuse(LRCNN_EINVAL, what, " is null");
   if ((uintptr_t)p & 3) return refuse(LRCNN_EINVAL, what, " is misaligned");

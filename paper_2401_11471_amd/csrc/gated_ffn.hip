@@ -120,6 +120,7 @@ extern "C" int lrcnn_gated_ffn_backward(int64_t rows, int64_t n_in, int64_t hidd
     TRY(take("dx", dx, lddx, n_in, es, true, &xm));
   }
   TRY(apart("duv", duv, {dz, w2t, dx ? w1t : nullptr}));
+  TRY(same_rows("duv", g.out, g.uv, rows));
   if (dx) TRY(apart("dx", dx, {duv, w1t}));
   g.rows = (int)rows, g.depth = (int)n_out, g.feats = (int)hidden, g.kind = kind;
   g.w = w.p;
