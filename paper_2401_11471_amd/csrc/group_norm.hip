@@ -949,6 +949,7 @@ extern "C" int lrcnn_group_norm_forward(int64_t batch, int64_t pixels, int64_t c
   GnArgs a{};
   TRY(take("x", x, ldx, channels, es, true, &a.x));
   TRY(take("y", y, ldy, channels, es, true, &a.y));
+  TRY(same_rows("y", a.y, a.x, batch * pixels));
   TRY(take_f32("gamma", gamma, false));
   TRY(take_f32("beta", beta, false));
   TRY(take_f32("mean", mean, false));
@@ -1006,6 +1007,8 @@ extern "C" int lrcnn_group_norm_backward(int64_t batch, int64_t pixels, int64_t 
     TRY(take("dy", dy, lddy, channels, es, true, &a.y));
     TRY(take("x", x, ldx, channels, es, false, &a.x));
     TRY(take("dx", dx, lddx, channels, es, true, &a.dx));
+    TRY(same_rows("dx", a.dx, a.y, batch * pixels));
+    TRY(same_rows("dx", a.dx, a.x, batch * pixels));
     TRY(take_f32("mean", mean, false));
     TRY(take_f32("rstd", rstd, true));
     TRY(take_f32("gamma", gamma, false));

@@ -27,3 +27,24 @@ def test_gated_ffn_backward_in_place_of_other_rows():
     # a stride too small is still that; no rows, nothing to refuse
     assert ffn_bwd(Q, 0, Q, 31) == ESHAPE
     assert ffn_bwd(Q, 0, Q, 40, rows=0) == 0
+
+
+def gn_fwd(x, ldx, y, ldy, batch=2, pixels=3):
+    return L.LIB.lrcnn_group_norm_forward(batch, pixels, 8, 2, L.F32, L.ACT_SILU, x, ldx, None,
+                                          None, 1e-5, y, ldy, None, None, None, P, 1 << 40, None)
+
+
+def gn_bwd(dy, lddy, x, ldx, dx, lddx, batch=2, pixels=3, ckpt=None):
+    return L.LIB.lrcnn_group_norm_backward(batch, pixels, 8, 2, L.F32, L.ACT_SILU, dy, lddy, x, ldx,
+                                           P if x else None, ckpt, P, None, None, dx, lddx, None,
+                                           None, 0, P, 1 << 40, None)
+
+
+def test_group_norm_in_place_of_other_rows():
+    for a, b in ((0, 16), (16, 0), (16, 24)):
+        refused(gn_fwd(Q, a, Q, b), "y")
+        refused(gn_bwd(Q, a, R, 0, Q, b), "dx")
+        refused(gn_bwd(Q, a, None, 0, Q, b, ckpt=R), "dx")
+        refused(gn_bwd(R, 0, Q, a, Q, b), "dx")
+    refused(gn_fwd(Q, 0, Q, 16, batch=1, pixels=2), "y")
+    assert gn_fwd(Q, 0, Q, 7) == ESHAPE and gn_bwd(Q, 0, R, 0, Q, 7) == ESHAPE
