@@ -95,6 +95,8 @@ extern "C" int lrcnn_dropout(int64_t rows, int64_t cols, int32_t dtype, const vo
   TRY(take("x", x, ldx, cols, es, true, &a.x));
   TRY(take("residual", residual, ldr, cols, es, false, &a.res));
   TRY(take("y", y, ldy, cols, es, true, &a.y));
+  TRY(same_rows("y", a.y, a.x, rows));
+  TRY(same_rows("y", a.y, a.res, rows));
   if (!rng) return refuse(LRCNN_EINVAL, "rng is null");
   if ((uintptr_t)rng & 7) return refuse(LRCNN_EINVAL, "rng is misaligned");
   a.rows = rows, a.cols = cols, a.vecs = vecs, a.first = first_row;

@@ -48,3 +48,16 @@ def test_group_norm_in_place_of_other_rows():
         refused(gn_bwd(R, 0, Q, a, Q, b), "dx")
     refused(gn_fwd(Q, 0, Q, 16, batch=1, pixels=2), "y")
     assert gn_fwd(Q, 0, Q, 7) == ESHAPE and gn_bwd(Q, 0, R, 0, Q, 7) == ESHAPE
+
+
+def drop(x, ldx, res, ldr, y, ldy, rows=2):
+    return L.LIB.lrcnn_dropout(rows, 8, L.F32, x, ldx, res, ldr, 0.5, P, 0, 0, y, ldy, None)
+
+
+def test_dropout_in_place_of_other_rows():
+    for a, b in ((0, 16), (16, 0), (16, 24)):
+        refused(drop(Q, a, None, 0, Q, b), "y")
+        refused(drop(Q, a, R, 0, Q, b), "y")
+        refused(drop(R, 0, Q, a, Q, b), "y")
+    assert drop(Q, 0, None, 0, Q, 7) == ESHAPE
+    assert drop(Q, 0, None, 0, Q, 16, rows=0) == 0
