@@ -27,7 +27,7 @@
 // corrected by the centred sum), then joined with
 //   n = na + nb, d = mb - ma, mean = ma + d nb / n, M2 = Ma + Mb + d^2 na nb / n,
 // so that a mean far from zero costs the variance no digits; across slabs
-// and channels in 64 bits.
+// and channels in 64 bits, as dgamma and dbeta across slabs and images.
 #include "activation.hpp"
 #include "kernels.hpp"
 
@@ -434,34 +434,41 @@ __global__ __launch_bounds__(1024) void gn_channel_kernel(GnArgs a, float2 *out)
   if (r == 0 && c < a.cols) out[(int64_t)b * a.cols + c] = make_float2((float)s1, (float)s2);
 }
 
-// dgamma and dbeta of 32 channels: thread (r, c) takes every 32nd unit from r on, the
-// 32 sums joined in order.
+// dgamma and dbeta of kChans channels: thread (r, c) takes every kRows-th unit from r
+// on, one wave joins a channel's sums of a kind. In 64 bits: a thread of the most images
+// adds 2^13 units, whose terms may cancel (262144 x 8 in float32: off by 7e-2 where the sum
+// is 1e4). Few channels a block, so that the conversions and the loads' latency are spread
+// (the whole backward pass with blocks of 32 channels and of 8: 51 x 5823 x 32 bf16 37.2 and
+// 35.0 us; with 32 and float32 sums 34.9, and 64 x 49 x 512 11.0 to 11.7 now).
+constexpr int kChans = 8, kRows = 1024 / kChans;
 __device__ __forceinline__ void channel_grads(const GnArgs &a, int block) {
-  __shared__ float l1[32][33], l2[32][33];
-  const int r = threadIdx.x >> 5, c = block * 32 + (threadIdx.x & 31);
-  float s1 = 0.f, s2 = 0.f;
+  __shared__ double l[2][kChans][kRows + 8];
+  const int r = threadIdx.x / kChans, x = threadIdx.x % kChans, c = block * kChans + x;
+  double s1 = 0, s2 = 0;
   if (c < a.cols) {
 #pragma unroll 8
-    for (int64_t u = r; u < a.units; u += 32) {
+    for (int64_t u = r; u < a.units; u += kRows) {
       const float2 v = a.part[u * a.cols + c];
       s1 += v.x, s2 += v.y;
     }
   }
-  l1[r][threadIdx.x & 31] = s1;
-  l2[r][threadIdx.x & 31] = s2;
+  l[0][x][r] = s1, l[1][x][r] = s2;
   __syncthreads();
-  if (r == 0 && c < a.cols) {
-    for (int k = 1; k < 32; ++k) s1 += l1[k][threadIdx.x], s2 += l2[k][threadIdx.x];
-    if (a.dbeta) a.dbeta[c] = a.accumulate ? a.dbeta[c] + s1 : s1;
-    if (a.dgamma) a.dgamma[c] = a.accumulate ? a.dgamma[c] + s2 : s2;
-  }
+  static_assert(kRows == 128 && 2 * kChans == 1024 / 64, "a wave joins 128 sums");
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, gamma = wave / kChans;
+  const int to = block * kChans + wave % kChans;
+  double s = l[gamma][wave % kChans][lane] + l[gamma][wave % kChans][lane + 64];
+#pragma unroll
+  for (int k = 1; k < 64; k *= 2) s += __shfl_xor(s, k);
+  float *const out = gamma ? a.dgamma : a.dbeta;
+  if (lane == 0 && to < a.cols && out) out[to] = (float)(a.accumulate ? out[to] + s : s);
 }
 __global__ __launch_bounds__(1024) void gn_grads_kernel(GnArgs a) {
   channel_grads(a, blockIdx.x);
 }
 
 // Block (image, group): a group's two means, of q and q xh; the blocks behind these:
-// the parameters' gradients of 32 channels each.
+// the parameters' gradients of kChans channels each.
 __global__ __launch_bounds__(1024) void gn_join_kernel(GnArgs a) {
   __shared__ double red[16];
   const int bg = a.batch * a.groups;
@@ -1022,7 +1029,7 @@ extern "C" int lrcnn_group_norm_backward(int64_t batch, int64_t pixels, int64_t 
   a.dgamma = dgamma, a.dbeta = dbeta, a.accumulate = accumulate != 0;
   a.k = ckpt_of(ckpt, batch * pixels, channels);
   hipStream_t s = (hipStream_t)stream;
-  const unsigned chans = (unsigned)up(channels, 32);
+  const unsigned chans = (unsigned)up(channels, kChans);
   if (!some) {  // no rows: the gradients are zero
     a.units = 0;
     gn_grads_kernel<<<chans, 1024, 0, s>>>(a);
