@@ -53,6 +53,18 @@ def held(x):
     return decode(*encode(x), x.shape[1])
 
 
+def misfits(q, e, ref, err):
+    """Where a checkpoint (codes, exponents) of values within err of ref cannot be right:
+    (groups, elements), truth values. A group's largest magnitude lies between those of
+    |ref| - err and |ref| + err, and its exponent between theirs, which are the same but next to
+    a power of two; a value stands within half of that exponent's step."""
+    ref, err = np.asarray(ref, np.float64), np.broadcast_to(err, np.shape(ref))
+    low, high = encode(np.maximum(np.abs(ref) - err, 0))[1], encode(np.abs(ref) + err)[1]
+    step = np.repeat(np.exp2(e.astype(np.float64) - 133), GROUP, 1)[:, :ref.shape[1]]
+    off = np.abs(decode(q, e, ref.shape[1]) - ref)
+    return (e < low) | (e > high), ~(off <= 0.5 * step + err)
+
+
 def pack_bytes(q, e):
     """The checkpoint's buffer: codes, then the exponents from the next multiple
     of 256 bytes (uint8)."""
