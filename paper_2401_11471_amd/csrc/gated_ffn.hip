@@ -11,9 +11,8 @@ std::atomic<int> g_ffn_tile{-1};
 
 namespace {
 
-int run(int32_t dtype, Epi epi, const FfnArgs &a, void *stream) {
-  return dtype == LRCNN_BF16 ? ffn_bf16(epi, a, (hipStream_t)stream)
-                             : ffn_f32(epi, a, (hipStream_t)stream);
+void run(int32_t dtype, Epi epi, const FfnArgs &a, void *stream) {
+  (dtype == LRCNN_BF16 ? ffn_bf16 : ffn_f32)(epi, a, (hipStream_t)stream);
 }
 
 // n: the block's input or output features. The products that this call makes with them
@@ -84,12 +83,12 @@ extern "C" int lrcnn_gated_ffn_forward(int64_t rows, int64_t n_in, int64_t hidde
   g.w = w.p, g.bias = b1;
   g.ku = ckpt_of(ckpt_u, rows, hidden);
   g.kv = ckpt_of(ckpt_v, rows, hidden);
-  TRY(run(dtype, EPI_GATE, g, stream));
+  run(dtype, EPI_GATE, g, stream);
   if (z) {
     FfnArgs d{};
     d.rows = (int)rows, d.depth = (int)hidden, d.feats = (int)n_out;
     d.x = g.out, d.w = w2m.p, d.bias = b2, d.out = zm;
-    TRY(run(dtype, EPI_PLAIN, d, stream));
+    run(dtype, EPI_PLAIN, d, stream);
   }
   return launched("gated_ffn_forward");
 }
@@ -127,12 +126,12 @@ extern "C" int lrcnn_gated_ffn_backward(int64_t rows, int64_t n_in, int64_t hidd
   g.ku = ckpt_of(ckpt_u, rows, hidden);
   g.kv = ckpt_of(ckpt_v, rows, hidden);
   g.ka = ckpt_of(ckpt_a, rows, hidden);
-  TRY(run(dtype, EPI_BACK, g, stream));
+  run(dtype, EPI_BACK, g, stream);
   if (dx) {
     FfnArgs d{};
     d.rows = (int)rows, d.depth = (int)(2 * hidden), d.feats = (int)n_in;
     d.x = g.out, d.w = w1m.p, d.out = xm;
-    TRY(run(dtype, EPI_PLAIN, d, stream));
+    run(dtype, EPI_PLAIN, d, stream);
   }
   return launched("gated_ffn_backward");
 }

@@ -46,8 +46,8 @@ struct FfnArgs {
 };
 
 // Products of one storage type (gated_ffn_bf16.hip, gated_ffn_f32.hip)
-int ffn_bf16(Epi epi, const FfnArgs &a, hipStream_t s);
-int ffn_f32(Epi epi, const FfnArgs &a, hipStream_t s);
+void ffn_bf16(Epi epi, const FfnArgs &a, hipStream_t s);
+void ffn_f32(Epi epi, const FfnArgs &a, hipStream_t s);
 extern std::atomic<int> g_ffn_tile;  // test hook: the variant to take where it can
 constexpr int64_t kMaxFeatures = 1 << 24, kMaxFfnRows = 1 << 30;
 // Tiles that a grid takes: fewer than 2^32 threads, 256 a tile. Calls have fewer than 2^22
@@ -102,7 +102,7 @@ __device__ __forceinline__ void strip_put(lds_char *l, int i, const f32x16 &b) {
 // Branches that end with different N stay apart, and their accumulators are stored from
 // where they are: joined, all are copied to the same registers first.
 template <int N>
-__device__ __forceinline__ void apart() {
+__device__ __forceinline__ void own_branch() {
   asm volatile("; strip %0" ::"n"(N));
 }
 template <int FB>
@@ -911,7 +911,7 @@ __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(F
       each<0, RB>([&](auto j_) {
         if (j == j_) {
           each<0, FB>([&](auto i) { strip_put<FB>(strip, i, acc[i][j_]); });
-          apart<j_>();
+          own_branch<j_>();
         }
       });
       wave_meets();
@@ -939,7 +939,7 @@ __global__ __launch_bounds__(256, W::LDS > 81920 ? 1 : 2) void ffn_wide_kernel(F
         constexpr int j = decltype(x)::value / 2, h = decltype(x)::value % 2;
         if (jh == x) {
           each<0, 2>([&](auto i) { strip_put<2>(strip, i, acc[2 * h + i][j]); });
-          apart<x>();
+          own_branch<x>();
         }
       });
       wave_meets();
@@ -1133,21 +1133,19 @@ void lay_out(FfnArgs &a, int rows, int feats) {
   a.rest = fast_div((uint32_t)std::max(a.gx & 7, 1));
 }
 template <typename T, typename TL, int EPI, bool DMA>
-int launch(FfnArgs &a, hipStream_t s) {
+void launch(FfnArgs &a, hipStream_t s) {
   lay_out(a, TL::R, EPI == EPI_GATE ? TL::F / 2 : TL::F);
   ffn_kernel<T, TL, EPI, DMA><<<(unsigned)(a.gx * a.gy), TL::THREADS, 0, s>>>(a);
-  return LRCNN_OK;
 }
 
 template <typename T, typename W, int EPI, bool DMA>
-int launch_wide(FfnArgs &a, hipStream_t s) {
+void launch_wide(FfnArgs &a, hipStream_t s) {
   lay_out(a, W::R, EPI == EPI_GATE ? W::F / 2 : W::F);
   ffn_wide_kernel<T, W, EPI, DMA><<<(unsigned)(a.gx * a.gy), 256, 0, s>>>(a);
-  return LRCNN_OK;
 }
 
 template <typename T, int EPI>
-int product(FfnArgs a, hipStream_t s) {
+void product(FfnArgs a, hipStream_t s) {
   constexpr int H = EPI == EPI_GATE ? 2 : 1;
   constexpr int kFew = 7;  // number of the variant for few rows; the others: costs below
   const int forced = g_ffn_tile;
@@ -1155,7 +1153,6 @@ int product(FfnArgs a, hipStream_t s) {
     auto few = [&](auto nc, auto nf) {
       const unsigned g = (unsigned)((a.feats + 16 * nf.value - 1) / (16 * nf.value));
       ffn_few_kernel<T, nc.value, EPI, nf.value><<<g, 512, 0, s>>>(a);
-      return LRCNN_OK;
     };
     using std::integral_constant;
     const integral_constant<int, 1> one;
@@ -1227,15 +1224,14 @@ int product(FfnArgs a, hipStream_t s) {
     case 4: return small(Small());
     case 5: return small(Tiny());
   }
-  if constexpr (EPI != EPI_GATE) return small(Least());
-  return LRCNN_OK;
+  if constexpr (EPI != EPI_GATE) small(Least());
 }
 
 template <typename T>
-int products_of(Epi epi, const FfnArgs &a, hipStream_t s) {
-  return epi == EPI_GATE   ? product<T, EPI_GATE>(a, s)
-         : epi == EPI_BACK ? product<T, EPI_BACK>(a, s)
-                           : product<T, EPI_PLAIN>(a, s);
+void products_of(Epi epi, const FfnArgs &a, hipStream_t s) {
+  if (epi == EPI_GATE) product<T, EPI_GATE>(a, s);
+  else if (epi == EPI_BACK) product<T, EPI_BACK>(a, s);
+  else product<T, EPI_PLAIN>(a, s);
 }
 
 }  // namespace

@@ -4,6 +4,6 @@
 
 namespace lrcnn {
 namespace act8 {
-int ffn_bf16(Epi epi, const FfnArgs &a, hipStream_t s) { return products_of<bf16>(epi, a, s); }
+void ffn_bf16(Epi epi, const FfnArgs &a, hipStream_t s) { products_of<bf16>(epi, a, s); }
 }  // namespace act8
 }  // namespace lrcnn

@@ -4,6 +4,6 @@
 
 namespace lrcnn {
 namespace act8 {
-int ffn_f32(Epi epi, const FfnArgs &a, hipStream_t s) { return products_of<float>(epi, a, s); }
+void ffn_f32(Epi epi, const FfnArgs &a, hipStream_t s) { products_of<float>(epi, a, s); }
 }  // namespace act8
 }  // namespace lrcnn
