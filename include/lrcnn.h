@@ -499,9 +499,9 @@ int lrcnn_group_norm_workspace_bytes(int64_t batch, int64_t pixels,
  * kind: f, an activation or LRCNN_ACT_NONE. gamma, beta: float32 [channels],
  * NULL for 1 and 0. mean, rstd: float32 [batch][groups], nullable. ckpt
  * (nullable): receives the checkpoint of xh, for lrcnn_group_norm_backward.
- * ESHAPE where groups does not divide channels, or beyond 2^20 images or
- * channels, 2^21 images times groups or 2^23 images times tiles of 512
- * channels. */
+ * Without images or pixels nothing is written. ESHAPE where groups does not
+ * divide channels, or beyond 2^20 images or channels, 2^21 images times groups
+ * or 2^23 images times tiles of 512 channels. */
 int lrcnn_group_norm_forward(int64_t batch, int64_t pixels, int64_t channels,
                              int64_t groups, int32_t dtype, int32_t kind,
                              const void *x, int64_t ldx, const float *gamma,
@@ -514,7 +514,9 @@ int lrcnn_group_norm_forward(int64_t batch, int64_t pixels, int64_t channels,
  *   e = dy * f'(gamma * xh + beta), q = gamma * e,
  *   dx = rstd * (q - mean(q) - xh * mean(q * xh)), means over the group,
  *   dgamma = sum over rows of e * xh, dbeta = sum over rows of e.
- * dgamma, dbeta: float32 [channels], each nullable. */
+ * dgamma, dbeta: float32 [channels], each nullable; their sums over slabs and
+ * images are in 64 bits. Without images or pixels they are zero, or where they are
+ * added to as they were. */
 int lrcnn_group_norm_backward(int64_t batch, int64_t pixels, int64_t channels,
                               int64_t groups, int32_t dtype, int32_t kind,
                               const void *dy, int64_t lddy, const void *x,
@@ -553,7 +555,7 @@ int lrcnn_dropout(int64_t rows, int64_t cols, int32_t dtype, const void *x,
  * and v; ckpt_u, ckpt_v the checkpoints of their float32 values. In place: z may
  * be x; a and uv may not, nor z a: EINVAL.
  * ESHAPE beyond 2^24 features or 2^30 rows, and from 2^22 tiles of 128 x 128 of
- * a product's result on. */
+ * x, [u v] or z on. */
 int lrcnn_gated_ffn_forward(int64_t rows, int64_t n_in, int64_t hidden,
                             int64_t n_out, int32_t dtype, int32_t kind,
                             const void *x, int64_t ldx, const void *w1,
@@ -572,7 +574,7 @@ int lrcnn_gated_ffn_forward(int64_t rows, int64_t n_in, int64_t hidden,
  * lrcnn_linear_wgrad's: of w2 from dz and ckpt_a, of w1 from duv and the
  * checkpoint of x. In place: duv may be uv (with uv's stride, else EINVAL), dx may be
  * dz or uv (not where that is duv), ckpt_a may be ckpt_u or ckpt_v; duv may not be
- * dz: EINVAL. ESHAPE as in the forward pass. */
+ * dz: EINVAL. ESHAPE as in the forward pass, by dz, [du dv] and dx. */
 int lrcnn_gated_ffn_backward(int64_t rows, int64_t n_in, int64_t hidden,
                              int64_t n_out, int32_t dtype, int32_t kind,
                              const void *dz, int64_t lddz, const void *w2t,

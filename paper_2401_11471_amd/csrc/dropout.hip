@@ -8,8 +8,9 @@
 // constant each round. One counter gives 128 bits, 16 for each of the eight
 // columns of a thread: the rounds' twenty wide products (a quarter of the rate of
 // others) then take less time than the row's bytes. Bound by HBM: 67800 x 2048 bf16 with
-// residual 144 us, 5.8 TB/s, at 0.14 vector instructions a cycle and SIMD; 392 x 512 float32
-// 2.7 us, a launch's time.
+// residual 143 to 150 us, 5.6 to 5.8 TB/s, at 0.14 vector instructions a cycle and SIMD; 392 x
+// 512 float32 2.7 us, a launch's time. Threads of a row are a power of two: of 199014 x 316
+// bf16, 40 vectors a row, 24 of 64 lanes are idle, 69 us against 42 at 6 TB/s.
 #include "act8.hpp"
 
 #include <type_traits>

@@ -9,13 +9,15 @@
 // operand: a lane then holds runs of four neighbouring features of one row, and u and v of
 // the same features are the same registers of two accumulators.
 //
-// 67800 x 2048 x 8192 bf16: forward 3.84 ms for the first kernel with both checkpoints (4.55
-// TFLOP, 1185 TFLOP/s; the library's product of its size alone 3.25), 1.70 for the second
-// (1340 TFLOP/s; 1.58); backward 2.60 and 3.42 ms (the library's products 1.57 and 3.12).
-// The plain products keep the matrix pipes 80% busy at 1.5 to 1.6 GHz, the clock that
-// their own power leaves; the first forward kernel 65% at 1.6, the first backward one 44% at
-// 1.9: of a tile's 57 and 76 us its results take 20 and 39, which one wave on a SIMD
-// doesn't overlap with products. Their vector instructions are 8 and 17 of them.
+// 67800 x 2048 x 8192 bf16, by the card: forward 3.70 to 3.98 ms for the first kernel with
+// both checkpoints (4.55 TFLOP, 1140 to 1230 TFLOP/s; the library's product of its size
+// alone 3.25 to 3.29), 1.66 to 1.72 for the second (1320 to 1370 TFLOP/s; 1.58 to 1.63);
+// backward 2.53 to 2.66 and 3.36 to 3.52 ms (the library's products 1.57 to 1.61 and 3.12 to
+// 3.17). Launch by launch in a trace, whose clocks vary more: up to 4.60 and 2.76 ms for the
+// first kernels. The plain products keep the matrix pipes 80% busy at 1.5 to 1.6 GHz,
+// the clock that their own power leaves; the first forward kernel 65% at 1.6, the first backward
+// one 44% at 1.9: of a tile's 57 and 76 us its results take 20 and 39, which one wave on a
+// SIMD doesn't overlap with products. Their vector instructions are 8 and 17 of them.
 #pragma once
 
 #include "activation.hpp"
@@ -1122,8 +1124,11 @@ typedef Wide<2, 2, 4> Deep;               // 128 x 128, one workgroup a CU
 typedef Tile<2, 2, 3> Small;              // 64 x 64
 typedef Tile<2, 1, 3> Tiny;               // 64 x 32
 typedef Tile<1, 1, 3> Least;              // 32 x 32, one block of features
-// (32 rows, few and the best tile, us: z of 2048 x 8192 bf16 23 and 31, 2048 x 512 float32
-// 12.5 and 29; first kernel 18.2 and 14.6, 11.4 and 11.9)
+// One limit for all products. 32 rows, few and the best tile, us: 2048 x 8192 bf16 z 23 and
+// 28, backward from checkpoints 12.8 and 12.4, dx 44 and 52; 512 x 2048 float32 z 12.5 and 29,
+// backward 8.7 and 8.8, dx 23 and 37. The forward pass' first kernel gains nothing (float32
+// 11.2 and 11.5) and loses in bfloat16 over a wide block: 18.2 and 14.6 at 32 rows, 17.1 and
+// 13.8 at 16, so there the limit is not the faster choice.
 constexpr int kFewRows = 32;
 
 void lay_out(FfnArgs &a, int rows, int feats) {
@@ -1172,10 +1177,13 @@ void product(FfnArgs a, hipStream_t s) {
                     Big::R * a.x.ld * (int64_t)sizeof(T) < (int64_t)1 << 32;
   // The variant of the least estimated time: for n tiles on the busiest of 256 CUs,
   // steps * max(alone, n * busy) + n * finish, in ns measured with one tile on a CU, with
-  // many, and for the results. (Measured by variant from 392 x 512 x 2048 to 67800 x 2048 x
-  // 8192, the pick is within a tenth of the best: 3136 x 1024 x 2736 bf16 in tiles of 256
-  // x 256, 256 x 128, 128 x 128 two and one a CU, 64 x 64, 64 x 32: first kernel 64, 59, 51,
-  // 64, 86, 92 us, z 56, 40, 34, 30, 49, 60; picked 52 and 30.)
+  // many, and for the results. Measured by variant at thirteen sizes from 33 x 2048 x 8192 and
+  // 392 x 512 x 2048 to 12000 x 512 x 2048, the pick is within 13% of the best (the first
+  // kernel of 256 x 2048 x 8192 24.3 us against 21.5, z of 2000 x 512 x 2048 13.8 against
+  // 12.2) and mostly within 5%: 3136 x 1024 x 2736 bf16 in tiles of 256 x 256, 256 x 128, 128
+  // x 128 two and one a CU, 64 x 64, 64 x 32: first kernel 64, 56, 48, 54, 77, 83 us, z 55, 40,
+  // 32, 28, 47, 57, backward 46, 49, 42, 47, 53, 59; picked 48, 29 and 42. (The times for the
+  // results are from before the strips' passes ran side by side: too long for some tiles.)
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int G = EPI == EPI_GATE ? 0 : EPI == EPI_BACK ? 1 : 2;
   struct Cost {

@@ -16,10 +16,11 @@
 // grouping, whatever the group's width and alignment, and in the backward pass both
 // the groups' means (weighted by gamma) and the parameters' gradients.
 //
-// Large maps are bound by HBM: 8 x 135000 x 512 bf16 with relu and checkpoint 235 us for the
-// sums (4.7 TB/s), 8 for the join, 532 for the result (5.2 TB/s); backward from the
-// checkpoint with silu, 8 x 8475 x 2048 bf16, 115 and 124 us (3.9 and 5.7 TB/s; the first
-// also by its vector instructions, 0.19 a cycle and SIMD). Small parts of a batch at a time,
+// Large maps are bound by HBM: 8 x 135000 x 512 bf16 with relu and checkpoint 238 to 256 us
+// for the sums (4.4 to 4.6 TB/s), 9 for the join, 530 to 543 for the result (5.2 TB/s);
+// backward from the checkpoint with silu, 8 x 8475 x 2048 bf16, 109 to 125 and 121 to 129 us
+// (3.6 to 4.1 and 5.7 TB/s; the first also by its vector instructions, 0.19 a cycle and
+// SIMD), from the map itself 285 in all. Small parts of a batch at a time,
 // so that the second pass finds the map in the Infinity Cache, took longer (1317 us and
 // 1078 with the unpack): what the pass before has written goes to memory meanwhile.
 //

@@ -21,7 +21,22 @@ updates and the weights' transposes are torch operations.
 
 ``fused``: a gated block's products run as two kernels a pass, the activation in the
 first one's registers: u and v then never exist at full width, and a is formed from their
-float32 values. ``dropout``: y = norm2(x + dropout(z)), whose mask is drawn again in the
+float32 values. Forward + backward pass in us, separate kernels and fused:
+
+====================  =======  ==============  =============
+block                 storage  separate        fused
+====================  =======  ==============  =============
+67800 x 2048 x 8192   bf16     13540 + 19680   5700 + 12780
+3136 x 1024 x 2736    bf16     156 + 262       91 + 214
+392 x 512 x 2048      float32  64 + 114        58 + 114
+256 x 2048 x 8192     bf16     83 + 189        64 + 220
+33 x 2048 x 8192      bf16     48 + 139        52 + 186
+1 x 2048 x 8192       bf16     43 + 129        34 + 114
+====================  =======  ==============  =============
+
+So fused is the choice from some 300 rows on and for a few; from 17 to some 300 rows of a
+wide block it is not where the block is trained: dx there has few tiles and a long depth,
+which fused products do not split over workgroups. The default is separate. ``dropout``: y = norm2(x + dropout(z)), whose mask is drawn again in the
 backward pass from the generator's state in device memory. ``GroupNorm`` normalises and
 activates the trunk's map in front of the block.
 
